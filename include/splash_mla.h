@@ -382,6 +382,144 @@ SPLASH_API int splash_dop_swap_outer(const void *in, int64_t A, int64_t B, int64
 SPLASH_API int splash_dop_unpack_rows(const void *recv, const int32_t *send_row, int64_t n, int64_t row_bytes,
                                       void *out, int64_t out_row_pitch, void *stream);
 
+/*
+ * ---- Keys and values in 8 bits --------------------------------------------------------------------------------------
+ *
+ * Serving a model whose layers keep keys and values per head (grouped-query attention), in pages of 64 tokens like the
+ * latent cache above: one e4m3 code per value and one fp32 scale for each page and key head.  Three calls make a step:
+ * splash_kv_slots gives the new tokens their places, splash_kv8_append writes their keys and values there,
+ * splash_kv8_attention attends over the cache.  (The paper has no counterpart; the layouts are those of the calls above: a
+ * head slice is a view of the pools, a request slice a call with fewer requests, a KV range kv_begin / kv_end, whose partial
+ * results splash_lse_merge combines.)
+ */
+
+/*
+ * Block tables and slot maps from the requests' lengths, on the device, so that a captured decode step needs no host for its
+ * bookkeeping.  Request i has seq_lens[i] tokens in the cache, in the pages of its table row, and gets new_lens[i] more
+ * (negative values count as 0).  The places of the batch's new tokens are numbered request after request,
+ *     q_start[i] = sum_{j < i} new_lens[j],  q_start has num_requests + 1 entries (sums above 2^31 - 1 are written as that),
+ * and the j-th new token of request i, place t = q_start[i] + j, gets
+ *     positions[t] = seq_lens[i] + j,
+ *     slot_map[t]  = 64 * block_table[i][positions[t] / 64] + positions[t] % 64.
+ * A page that the request has not yet begun comes from the free list: requests in their order take the pages
+ * free_pages[free_begin[0]], free_pages[free_begin[0] + 1], ... and their table rows get the ids (page ids are copied, not
+ * checked).  new_seq_lens[i] = seq_lens[i] + new_lens[i].
+ *
+ * A request is served whole or not at all.  Refused is one whose tokens would not fit its table row (table_width entries) or
+ * 2^31 - 1 tokens, whose places end behind num_slots, or for which too few free pages are left; once a request is refused for
+ * want of pages, so is every later one that needs a page.  A refused request keeps its length and its table row, and its places hold -1 in slot_map and
+ * positions; so do the places in [q_start[num_requests], num_slots) (a padded batch).  q_start counts its tokens all the same.
+ *     counts[0] = q_start[num_requests], counts[1] = pages taken, counts[2] = requests refused,
+ *     counts[3] = free_begin[0] + pages taken, the free_begin of the next call.
+ *
+ *   seq_lens, new_lens  [num_requests] int32;  num_requests <= SPLASH_KV_SLOTS_MAX_REQUESTS
+ *   free_pages          [num_free] int32;  free_begin [1] int32 (outside [0, num_free]: no page is free)
+ *   block_table         [num_requests][block_table_stride] int32, the first table_width entries of a row are used; only the
+ *                       entries of new pages are written
+ *   slot_map [num_slots] int64, positions [num_slots] int32, q_start [num_requests + 1], new_seq_lens [num_requests],
+ *   counts [4] int32    outputs; none may overlap another one, an input or the table
+ */
+#define SPLASH_KV_SLOTS_MAX_REQUESTS 16384
+SPLASH_API int splash_kv_slots(int32_t num_requests, const int32_t *seq_lens, const int32_t *new_lens,
+                               const int32_t *free_pages, int64_t num_free, const int32_t *free_begin,
+                               int32_t *block_table, int64_t block_table_stride, int32_t table_width, int64_t num_slots,
+                               int64_t *slot_map, int32_t *positions, int32_t *q_start, int32_t *new_seq_lens, int32_t *counts,
+                               void *stream);
+
+enum { SPLASH_DTYPE_BF16 = 0, SPLASH_DTYPE_FP16 = 1, SPLASH_DTYPE_FP32 = 2 };
+
+/*
+ * A cache of keys and values in e4m3.  The code of token offset r of page p, head h, dimension d lies at byte
+ *     k_pool + p * k_page_stride + h * k_head_stride + r * head_dim + d       (values alike)
+ * and stands for code * k_scales[p * k_scale_stride + h].  The rows of a (page, head) are dense.  Strides are in bytes for the
+ * pools, multiples of 16; in elements for the scales.  A rank's head slice is the same struct with the pointers moved to
+ * its first head.
+ */
+typedef struct splash_kv8_cache {
+    uint32_t struct_size;        /* sizeof(splash_kv8_cache) */
+    int32_t num_pages;           /* pages addressable from the pools */
+    int32_t num_kv_heads;        /* 1..65,535 */
+    int32_t head_dim;            /* 64 or 128 */
+    int32_t page_size;           /* 64 tokens */
+    int32_t reserved;            /* 0 */
+    void *k_pool, *v_pool;       /* 16-byte aligned */
+    float *k_scales, *v_scales;
+    int64_t k_page_stride, k_head_stride, v_page_stride, v_head_stride;
+    int64_t k_scale_stride, v_scale_stride;   /* from page to page; >= num_kv_heads */
+} splash_kv8_cache;
+
+/*
+ * Write keys and values into the cache: row j of k and v, [num_rows][num_kv_heads][head_dim] bf16 or fp16, goes to the place
+ * slot_map[j] = 64 * page + offset (splash_kv_slots' map).  A row whose slot is negative or names no page of the cache is skipped.
+ * A run of rows with ascending consecutive slots inside one page is written as one.  With a = max |x| over the run's finite values of a head, and
+ *     need = the smallest power of two with a <= 448 * need, at least 2^-100,
+ * the (page, head)'s scale s becomes need for a run that begins at offset 0, and for a run behind older rows max(s, need); the
+ * codes are c = e4m3(x / s), rounded to nearest even.  Powers of two make that division exact: an older code that moves to
+ * a larger scale, c' = e4m3(c * s / s'), changes only where it leaves the normal range, and a result does not depend on how
+ * a context was cut into calls but for that.  (A scale in the cache that is no power of two, of a page filled elsewhere, is
+ * kept while it suffices, x / s is then rounded to fp32 first; one that is NaN is replaced.)  Infinities and NaN are stored as NaN.  Rows of the page behind the
+ * run are left as they are: they belong to no token.
+ *
+ * The rows of a page must form ONE run of the call, and no two requests may share a page that is written (copy a shared page
+ * first); what such a page then holds is undefined, nothing else is touched.
+ * Strides of k and v are in elements, multiples of 8; both 16-byte aligned; rows dense in the last dimension.
+ */
+SPLASH_API int splash_kv8_append(const splash_kv8_cache *cache, int32_t dtype, int64_t num_rows,
+                                 const void *k, int64_t k_row_stride, int64_t k_head_stride,
+                                 const void *v, int64_t v_row_stride, int64_t v_head_stride,
+                                 const int64_t *slot_map, void *stream);
+
+/*
+ * Attention over that cache.  Strides are in ELEMENTS of the array they index.
+ *   q   : dtype,     row t, head g, dimension d at q  [t * q_row_stride   + g * q_head_stride   + d]
+ *   out : out_dtype, the same                    at out[t * out_row_stride + g * out_head_stride + d]
+ *   lse : fp32,      row t, head g               at lse[t * lse_row_stride + g]
+ */
+typedef struct splash_kv8_query {
+    uint32_t struct_size;        /* sizeof(splash_kv8_query) */
+    int32_t num_requests;        /* B >= 0 */
+    int64_t num_rows;            /* T: rows of q, out and lse; below 2^31 */
+    int32_t num_heads;           /* a multiple of the cache's num_kv_heads, at most 1,024 heads for each; head g reads key head g / (num_heads / num_kv_heads) */
+    int32_t max_q_rows;          /* upper bound on the rows of a request, >= 1 */
+    int32_t dtype;               /* of q: SPLASH_DTYPE_BF16 or SPLASH_DTYPE_FP16 */
+    int32_t out_dtype;           /* that of q, or SPLASH_DTYPE_FP32 (partial results that are merged) */
+    int64_t q_row_stride, q_head_stride;       /* multiples of 8 */
+    int64_t out_row_stride, out_head_stride;   /* multiples of 8 */
+    int64_t lse_row_stride;
+    int64_t block_table_stride;  /* entries from one request's row of block_table to the next */
+    int32_t table_width;         /* entries of a row that may be read: a context is cut at 64 * table_width tokens */
+    float softmax_scale;
+} splash_kv8_query;
+
+/*
+ * Request i has the n = q_start[i + 1] - q_start[i] query rows q_start[i] .. q_start[i + 1] - 1 (q_start = NULL: one row each, row
+ * i, num_rows = num_requests).  They are its n newest tokens, whose keys and values are in the cache already: row r sits at
+ * position seq_lens[i] - n + r and attends the tokens
+ *     R = [max(0, kv_begin[i]), min(kv_end[i], seq_lens[i] - n + r + 1)),
+ *     l_t = softmax_scale * q . K_t,  lse = ln sum_{t in R} exp(l_t),  out = sum_{t in R} exp(l_t - lse) V_t
+ * over the dequantised keys and values of its key head.  An empty R gives out = 0, lse = -inf.  Rows of q that belong to no
+ * request (behind q_start[num_requests] in a padded batch) are not read and their outputs are left as they were; a request's rows beyond max_q_rows
+ * or num_rows alike.
+ *
+ * Only tokens in R enter a row's result: codes of the cache's other places, and scales of pages without a token of R, may be
+ * anything, NaN included; NaN in a token's data stays NaN in the rows that attend it.  A page id outside the
+ * cache is never dereferenced, the page reads as zeros.  Products are exact (8-bit codes times q, which is scaled to fp16's range by a power of two per
+ * row) and summed in fp32; softmax weights are rounded to fp16 relative to the row's running maximum, maxima and sums are
+ * fp32.  Value scales that differ by up to 2^29 between the pages of a request keep that precision.  Results are bit-reproducible for a fixed call.
+ *
+ *   block_table  [num_requests][block_table_stride] int32;  seq_lens, kv_begin, kv_end [num_requests] int32 (the latter two
+ *                or NULL);  q_start [num_requests + 1] int32, ascending, or NULL
+ *   workspace    at least splash_kv8_attention_workspace_bytes() bytes, 256-byte aligned; two calls that may overlap on the
+ *                device need different ones.  splash_workspace_status reads its status word.
+ */
+SPLASH_API int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *query, const void *q,
+                                    const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_start,
+                                    const int32_t *kv_begin, const int32_t *kv_end, void *out, float *lse,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace size for splash_kv8_attention (host computation); depends on head_dim and the device's SM count only.  Returns 0 on invalid arguments. */
+SPLASH_API size_t splash_kv8_attention_workspace_bytes(const splash_kv8_cache *cache, const splash_kv8_query *query);
+
 /* Host-side helpers. */
 SPLASH_API const char *splash_status_string(int status);
 SPLASH_API const char *splash_last_error(void);

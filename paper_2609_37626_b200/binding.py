@@ -4,8 +4,8 @@ the library's CUDA kernels.  There is no fallback: if the shared library has not
 been built the use of its symbols fails loudly.
 
 The calls of a serving loop (splash_mla_decode, splash_mla_decode_sparse,
-splash_lse_merge, splash_kv_page_migrate and its static form, splash_dop_*) are
-functions of the extension module ``_splash_torch``, which reads the tensors in
+splash_lse_merge, splash_kv_page_migrate and its static form, splash_dop_*,
+splash_kv_slots, splash_kv8_*) are functions of the extension module ``_splash_torch``, which reads the tensors in
 C++; the rest goes through ctypes.
 """
 from __future__ import annotations
@@ -71,6 +71,33 @@ class MlaShape(ctypes.Structure):
     ]
 
 
+class Kv8Cache(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("num_pages", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+        ("k_page_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64), ("v_page_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+        ("k_scale_stride", ctypes.c_int64), ("v_scale_stride", ctypes.c_int64),
+    ]
+
+
+class Kv8Query(ctypes.Structure):
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("num_requests", ctypes.c_int32),
+        ("num_rows", ctypes.c_int64),
+        ("num_heads", ctypes.c_int32), ("max_q_rows", ctypes.c_int32), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+        ("q_row_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+        ("lse_row_stride", ctypes.c_int64),
+        ("block_table_stride", ctypes.c_int64),
+        ("table_width", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+    ]
+
+
 class MigrateJob(ctypes.Structure):
     _fields_ = [
         ("struct_size", ctypes.c_uint32),
@@ -126,6 +153,14 @@ def load() -> ctypes.CDLL:
     lib.splash_dop_swap_outer.argtypes = [vp, i64, i64, i64, vp, vp]
     lib.splash_dop_unpack_rows.restype = ctypes.c_int
     lib.splash_dop_unpack_rows.argtypes = [vp, vp, i64, i64, vp, i64, vp]
+    lib.splash_kv_slots.restype = ctypes.c_int
+    lib.splash_kv_slots.argtypes = [i32, vp, vp, vp, i64, vp, vp, i64, i32, i64, vp, vp, vp, vp, vp, vp]
+    lib.splash_kv8_append.restype = ctypes.c_int
+    lib.splash_kv8_append.argtypes = [ctypes.POINTER(Kv8Cache), i32, i64, vp, i64, i64, vp, i64, i64, vp, vp]
+    lib.splash_kv8_attention.restype = ctypes.c_int
+    lib.splash_kv8_attention.argtypes = [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8Query), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.splash_kv8_attention_workspace_bytes.restype = sz
+    lib.splash_kv8_attention_workspace_bytes.argtypes = [ctypes.POINTER(Kv8Cache), ctypes.POINTER(Kv8Query)]
     lib.splash_status_string.restype = ctypes.c_char_p
     lib.splash_status_string.argtypes = [ctypes.c_int]
     lib.splash_last_error.restype = ctypes.c_char_p
@@ -183,7 +218,8 @@ def splash_mla_decode_workspace_bytes(shape: MlaShape, head_begin: int, head_end
 
 # ---- the extension module ----------------------------------------------------------
 _NATIVE = ("splash_mla_decode", "splash_mla_decode_sparse", "splash_lse_merge", "splash_kv_page_migrate",
-           "splash_kv_page_migrate_static", "splash_dop_pack_rows", "splash_dop_swap_outer", "splash_dop_unpack_rows")
+           "splash_kv_page_migrate_static", "splash_dop_pack_rows", "splash_dop_swap_outer", "splash_dop_unpack_rows",
+           "splash_kv_slots", "splash_kv8_append", "splash_kv8_attention")
 _ext = None
 
 
@@ -205,6 +241,8 @@ def _load_ext():
     _ext = ext
     _ext.set_error_class(SplashError)
     for name in _NATIVE:
+        if not hasattr(_ext, name):
+            raise ImportError(f"{path} is older than this module (it has no {name}): build it with `python -m {__package__}.build`")
         globals()[name] = getattr(_ext, name)
     return _ext
 

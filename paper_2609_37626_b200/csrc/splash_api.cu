@@ -135,6 +135,16 @@ void set_error(const char *fmt, ...) {
 
 void count_launch(int n) { g_launches += n; }
 
+void begin_call() { g_launches = 0; }
+
+int usable_device(int &sm_count) {
+    DeviceInfo dev;
+    if (!current_device_info(dev)) return SPLASH_CUDA_ERROR;
+    if (dev.cc_major != 10) { set_error("device compute capability %d.x is not 10.x", dev.cc_major); return SPLASH_UNSUPPORTED_DEVICE; }
+    sm_count = dev.sm_count;
+    return SPLASH_OK;
+}
+
 }  // namespace splash
 
 using namespace splash;

@@ -483,6 +483,8 @@ struct DeviceOnce {
 // ---- host helpers (splash_api.cu) -----------------------------------------
 void set_error(const char *fmt, ...);
 void count_launch(int n = 1);
+void begin_call();                       // a call's launches are counted from here
+int usable_device(int &sm_count);        // SPLASH_OK and the current device's SM count, or the status of a device that the kernels do not run on
 
 // kernels' host launchers
 cudaError_t launch_plan(const DecodeParams &p, const PlanView &v, cudaStream_t stream);

@@ -1,0 +1,730 @@
+// Attention of few query rows over a paged cache of keys and values in e4m3 with a scale per (page, head).
+//
+// For a key head the query rows of a request and the heads of the group form (row, head) pairs, m = row * group + head, cut in tiles of
+// 16 or 32.  An item of work is (request, key head, tile); its pages are streamed once:
+//     x = q . K * softmax_scale * log2 e * k_scale,  p = 2^(x - m + 7),  l += p,  O += p * v_scale / U * V
+// with a reference m per row that moves only when a logit exceeds it by 8 (then O and l are rescaled) and U the largest
+// value scale so far.  p <= 2^15 is rounded to fp16 for the product with V: 11 bits at any length of context, weights down to
+// 2^-29 of the largest one keep them.  Queries are scaled to fp16's range by a power of two per row, so that bf16 ones lose nothing.
+//
+// The cache's bytes bound it: 16 KB a page and head against 128 mma.m16n8k16.  What it takes to stay there:
+//   - items are cut where the cost line (pages, and kOverhead per item) of all requests passes a worker's share, so one long
+//     context and 512 short ones fill the SMs alike; cut items are joined by a combine kernel.  Two workers per SM.
+//   - a producer warp walks the line, 32 pages at once: a lane each finds its page, its scales and its flags; TMA brings
+//     keys and values (swizzled against bank conflicts), four or eight pages ahead, across items;
+//   - four warps take 16 tokens of every page each, with their own m, l, O: they meet only at the end of an item;
+//   - the order of dimensions within an MMA's k does not matter if both operands agree, nor the order of tokens: a lane reads
+//     its key and value codes 16 bytes at a time and widens them in registers (e4m3 -> fp16 is exact).  Keys: lane (n, c) of the fragment takes
+//     token perm(n) and the 16-byte chunks c, c + 4 of its row, which are the values of the k slots 2c, 2c + 1, 2c + 8, 2c + 9 of successive
+//     MMAs; values: tokens c, c + 4, c + 8, c + 12 and the chunk perm(n), bytes of two tokens interleaved.
+// mma.sync and not tcgen05: with at most 32 rows the MMAs take a fifth of the time that the bytes take, and the 8-bit
+// operands would have to be widened into shared memory first, twice the bytes over the path that is next in line.
+#include "splash_kv8.cuh"
+#include "splash_umma.cuh"
+
+namespace splash {
+
+namespace {
+
+using namespace kv8;
+using namespace umma;
+
+constexpr int kConsumers = 4;                       // warps, 16 tokens of a page each
+constexpr int kThreads = 32 * (kConsumers + 1);
+constexpr int kOverhead = 2;                        // cost of an item beside its pages, in pages
+constexpr int kMinUnits = 2;                        // least cost of a worker's share
+constexpr float kLift = 7.f, kSlack = 8.f;          // weights are kept below 2^(kLift + kSlack) = 2^15
+
+enum { kFirst = 1, kLast = 2, kEmpty = 4, kEnd = 8, kEdge = 16, kCausal = 32 };
+
+// What the consumers need to know about a page in the ring, written by the producer.
+struct alignas(16) PageInfo {
+    int row0, rows_all, pairs, m0;      // the item's rows
+    int head, len, lo, hi;              // key head; context; the request's token range
+    int t0, flags, slot, pad;           // first token of the page; partial slot or -1
+    float k_scale, v_scale;
+    int pad2[2];
+};
+
+template <int D, int MT>
+struct Layout {
+    static constexpr int kRows = 16 * MT;
+    static constexpr int kStages = D == 128 ? 4 : 8;
+    static constexpr int kHalf = 64 * D;                                   // keys or values of a page
+    static constexpr int kPad = D + 4;
+    static constexpr int kMerge = kStages * 2 * kHalf;                     // [4][16][D + 4] fp32
+    static constexpr int kQuery = kMerge + kConsumers * 16 * kPad * 4;     // MT > 1: [MT][D / 16][32] uint4
+    static constexpr int kInfo = kQuery + (MT > 1 ? MT * (D / 16) * 512 : 0);
+    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // m, l: [4][rows] each
+    static constexpr int kBars = kStats + 2 * 2 * kConsumers * kRows * 4;  // (two sets)
+    static constexpr int kBytes = kBars + (2 * kStages + 1) * 8 + 1024;    // (the start is aligned to 1,024)
+};
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16-byte chunk `chunk` of row `row` of a [64][D] tile as the TMA unit has swizzled it
+template <int D>
+__device__ __forceinline__ uint32_t chunk_at(int row, int chunk) {
+    return D == 128 ? row * 128 + ((chunk ^ (row & 7)) << 4) : row * 64 + ((chunk ^ (row >> 1 & 3)) << 4);
+}
+
+// 16 query values from dimension d on, as fp32
+__device__ __forceinline__ void load_q16(const AttnParams &p, int64_t at, bool there, float (&v)[16]) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (there) w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.q) + at + half * 8);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float2 f;
+            if (p.q_bf16) f = make_float2(__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xffff0000u));
+            else f = __half22float2(*reinterpret_cast<const __half2 *>(&u[k]));
+            v[half * 8 + 2 * k] = f.x; v[half * 8 + 2 * k + 1] = f.y;
+        }
+    }
+}
+
+// Units of the cost line: (kOverhead + pages) for each (key head, tile) of a request that is this kernel's.
+template <int kRows>
+__device__ __forceinline__ int64_t units_of(const AttnParams &p, const Request &r) {
+    if (r.pairs < p.min_pairs || r.pairs > p.max_pairs || r.pairs == 0) return 0;
+    return (int64_t)p.kv_heads * ((r.pairs + kRows - 1) / kRows) * (kOverhead + r.pages());
+}
+
+struct Share { int64_t begin, end, total, u0; int i0, workers; };
+
+// The worker's share of the cost line and where it begins: request i0, unit u0 of it.  All threads.
+template <int kRows>
+__device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
+    __shared__ int64_t sums[kThreads / 32];
+    __shared__ int64_t found_u;
+    __shared__ int found_i;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.B + kThreads - 1) / kThreads, i0 = min(tid * per, p.B), i1 = min(i0 + per, p.B);
+    int64_t mine = 0;
+    for (int i = i0; i < i1; ++i) mine += units_of<kRows>(p, request(p, i));
+    int64_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += x;
+    }
+    if (lane == 31) sums[warp] = sum;
+    __syncthreads();
+    Share s;
+    s.total = 0;
+    int64_t before = sum - mine;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) before += sums[w];
+        s.total += sums[w];
+    }
+    s.workers = (int)max((int64_t)1, min((int64_t)p.workers, s.total / kMinUnits));
+    s.begin = worker < s.workers ? s.total * worker / s.workers : s.total;
+    s.end = worker < s.workers ? s.total * (worker + 1) / s.workers : s.total;
+    if (before <= s.begin && s.begin < before + mine) {
+        int64_t u = s.begin - before;
+        int i = i0;
+        for (; i < i1; ++i) {
+            const int64_t n = units_of<kRows>(p, request(p, i));
+            if (u < n) break;
+            u -= n;
+        }
+        found_i = i;
+        found_u = u;
+    }
+    __syncthreads();
+    s.i0 = s.begin < s.total ? found_i : p.B;
+    s.u0 = s.begin < s.total ? found_u : 0;
+    return s;
+}
+
+template <int D, int MT>
+__device__ __forceinline__ void produce(const AttnParams &p, const Share &share, const CUtensorMap *k_map, const CUtensorMap *v_map, uint8_t *smem, uint32_t bars,
+                                        const Ctx &ctx, int worker, int lane) {
+    using L = Layout<D, MT>;
+    const uint32_t full = bars, empty = bars + 8 * L::kStages;
+    PageInfo *const info = reinterpret_cast<PageInfo *>(smem + L::kInfo);
+    int stage = 0, i = share.i0;
+    uint32_t phase = 0;
+    int64_t unit = share.begin, u = share.u0;
+    bool ok = true, has_cut = false, more = share.begin < share.end;
+    while (more && ok) {
+        // every lane: its unit's item, page and scales
+        const int64_t mine = unit + lane;
+        int64_t lu = u + lane;
+        int li = i;
+        Request r = {};
+        int64_t n = 0;
+        for (; li < p.B; ++li) {
+            r = request(p, li);
+            n = units_of<L::kRows>(p, r);
+            if (lu < n) break;
+            lu -= n;
+        }
+        const bool exists = li < p.B;
+        const int pages = r.pages(), cost = kOverhead + pages;
+        const int sub = exists ? (int)(lu / cost) : 0, pos = exists ? (int)(lu - (int64_t)sub * cost) : 0;
+        const int tiles = (r.pairs + L::kRows - 1) / L::kRows;
+        const int64_t item = mine - pos;                       // the item's place on the line
+        const bool done = !exists || (p.whole ? item >= share.end : mine >= share.end);
+        const bool ours = !done && (!p.whole || item >= share.begin);
+        const bool data = ours && pos >= kOverhead, blank = ours && pages == 0 && pos == 0;
+        const bool cut_front = !p.whole && item + kOverhead < share.begin, cut_back = !p.whole && item + cost > share.end;
+        PageInfo a = {};
+        int id = 0;
+        bool valid = false;
+        if (data) {
+            const int page = r.lo / kPage + pos - kOverhead;
+            id = load_l2(p.table + li * p.table_stride + page);
+            valid = id >= 0 && id < p.num_pages;
+            a.t0 = page * kPage;
+        }
+        a.row0 = r.row0; a.rows_all = r.rows_all; a.pairs = r.pairs; a.m0 = exists ? (sub % tiles) * L::kRows : 0;
+        a.head = exists ? sub / tiles : 0; a.len = r.len; a.lo = r.lo; a.hi = r.hi;
+        a.slot = cut_front ? 2 * worker : cut_back ? 2 * worker + 1 : -1;
+        a.k_scale = valid ? p.k_scales[id * p.k_scale_stride + a.head] : 0.f;
+        a.v_scale = valid ? p.v_scales[id * p.v_scale_stride + a.head] : 0.f;
+        if (isinf(a.v_scale)) a.v_scale = NAN;
+        if (data) {
+            if (pos == kOverhead || mine == share.begin) a.flags |= kFirst;
+            if (pos == cost - 1 || (!p.whole && mine == share.end - 1)) a.flags |= kLast;
+            // tokens outside the range, or hidden from some of the rows
+            if (a.t0 < r.lo || a.t0 + kPage > r.hi) a.flags |= kEdge;
+            if (a.t0 + kPage > r.len - r.rows_all + 1) a.flags |= r.rows_all > 1 ? kEdge | kCausal : kEdge;
+        } else {
+            a.flags = kEmpty;
+        }
+        if (data && pos == kOverhead && cut_back) {
+            // the item's last worker is the one whose share holds its last unit
+            const int last = (int)(((item + cost) * share.workers - 1) / share.total);
+            p.cut[worker] = make_int4(li, sub, last - worker + 1, 0);
+        }
+        has_cut |= __any_sync(0xffffffffu, data && pos == kOverhead && cut_back);
+        unsigned todo = __ballot_sync(0xffffffffu, data || blank);
+        while (todo != 0) {
+            const int j = __ffs(todo) - 1;
+            todo &= todo - 1;
+            ok = warp_wait(ctx, empty + 8 * stage, phase ^ 1, 100 + stage);
+            if (!ok) break;
+            if (lane == j) {
+                info[stage] = a;
+                if (data) {
+                    const uint32_t dst = smem_u32(smem) + stage * 2 * L::kHalf;
+                    mbar_expect_tx(full + 8 * stage, 2 * L::kHalf);
+                    tma_load_4d(dst, k_map, full + 8 * stage, 0, 0, a.head, valid ? id : p.num_pages);      // (behind the pool: zeros)
+                    tma_load_4d(dst + L::kHalf, v_map, full + 8 * stage, 0, 0, a.head, valid ? id : p.num_pages);
+                } else {
+                    mbar_arrive(full + 8 * stage);
+                }
+            }
+            __syncwarp();
+            if (++stage == L::kStages) { stage = 0; phase ^= 1; }
+        }
+        more = !__shfl_sync(0xffffffffu, (int)done, 31);
+        i = __shfl_sync(0xffffffffu, li, 31);
+        u = __shfl_sync(0xffffffffu, lu, 31) + 1;
+        unit += 32;
+    }
+    if (ok) ok = warp_wait(ctx, empty + 8 * stage, phase ^ 1, 120);
+    if (ok && lane == 0) {
+        info[stage].flags = kEnd;
+        mbar_arrive(full + 8 * stage);
+    }
+    if (!p.whole && !has_cut && lane == 0) p.cut[worker] = make_int4(0, 0, 0, 0);
+    if (!ok) {
+        // a wait has given up: the copies still in flight must land before the block's shared memory goes to another one
+        for (int s = 0; s < L::kStages; ++s) {
+            const uint32_t parity = s < stage ? phase : phase ^ 1;         // of the stage's last use
+            for (int k = 0; k < 100000 && !mbar_test_wait(full + 8 * s, parity); ++k) {}
+        }
+    }
+}
+
+// All consumer warps meet; false: one of them has given up.
+__device__ __forceinline__ bool meet(const Ctx &ctx, uint32_t bar, uint32_t &phase, int lane) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+    const bool ok = warp_wait(ctx, bar, phase, 130);
+    phase ^= 1;
+    return ok;
+}
+
+__device__ __forceinline__ void store4(const AttnParams &p, int64_t at, const float4 &v) {
+    if (p.out_f32) {
+        *reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at) = v;
+    } else {
+        const uint2 h = p.q_bf16 ? make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)) : make_uint2(pack_f16x2(v.x, v.y), pack_f16x2(v.z, v.w));
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + at) = h;
+    }
+}
+
+template <int D, int MT>
+__device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint32_t bars, const Ctx &ctx, int warp, int lane) {
+    using L = Layout<D, MT>;
+    constexpr int kK = D / 16, kN = D / 8;                  // MMAs along the dimensions: as k of the logits, as n of the outputs
+    const uint32_t full = bars, empty = bars + 8 * L::kStages, group_bar = bars + 16 * L::kStages;
+    const PageInfo *const infos = reinterpret_cast<const PageInfo *>(smem + L::kInfo);
+    float *const merge = reinterpret_cast<float *>(smem + L::kMerge);
+    uint4 *const query = reinterpret_cast<uint4 *>(smem + L::kQuery);
+    // m and l of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
+    float *stat_m = reinterpret_cast<float *>(smem + L::kStats);
+    const int n = lane >> 2, c = lane & 3;
+    const int perm = D == 128 ? (n >> 1) | (n & 1) << 2 : n;
+    const int tok_a = D == 128 ? c : 2 * c, tok_b = D == 128 ? c + 4 : 2 * c + 1;     // tokens of the S columns 2c, 2c + 1
+
+    float o[MT][kN][4], m[MT][2], l[MT][2], rs[MT][2], unit = 0.f;
+    uint32_t qf[MT == 1 ? kK : 1][4];
+    int lim[MT][2];
+    int stage = 0;
+    uint32_t phase = 0, group_phase = 0;
+    for (;;) {
+        if (!warp_wait(ctx, full + 8 * stage, phase, 140 + stage)) break;
+        const PageInfo &info = infos[stage];
+        const int flags = info.flags;
+        if (flags & kEnd) break;
+        if (flags & (kFirst | kEmpty)) {
+            // the item's queries, as fp16 with a power of two per row that brings the largest of a row to [2^14, 2^15)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                float v[2][D / 64][16];
+                float factor[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int mm = info.m0 + mt * 16 + n + 8 * e;
+                    const bool there = mm < info.pairs && !(flags & kEmpty);
+                    const int row = mm / p.group, g = mm - row * p.group;
+                    const int64_t at = (info.row0 + row) * p.q_row + (info.head * p.group + g) * p.q_head;
+                    lim[mt][e] = there ? min(info.hi, info.len - info.rows_all + row + 1) : info.hi;
+                    int most = 0;
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h) {
+                        load_q16(p, at + h * 64 + 16 * c, there, v[e][h]);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const int b = __float_as_int(v[e][h][k]) & 0x7fffffff;
+                            if (b < 0x7f800000) most = max(most, b);
+                        }
+                    }
+                    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                    const int shift = most == 0 ? 0 : min(14 - ((most >> 23) - 127), 100);
+                    factor[e] = __int_as_float((shift + 127) << 23);
+                    rs[mt][e] = p.scale_log2 * __int_as_float((127 - shift) << 23);
+                    m[mt][e] = -INFINITY;
+                    l[mt][e] = 0.f;
+                }
+#pragma unroll
+                for (int k = 0; k < kK; ++k) {
+                    const int h = k / 4, at = 4 * (k % 4);
+                    uint32_t a[4];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        a[e] = pack_f16x2(v[e][h][at] * factor[e], v[e][h][at + 1] * factor[e]);
+                        a[2 + e] = pack_f16x2(v[e][h][at + 2] * factor[e], v[e][h][at + 3] * factor[e]);
+                    }
+                    if constexpr (MT == 1) {
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) qf[k][x] = a[x];
+                    } else if (k % kConsumers == warp) {
+                        query[(mt * kK + k) * 32 + lane] = make_uint4(a[0], a[1], a[2], a[3]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kN; ++j)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[mt][j][x] = 0.f;
+            }
+            unit = 0.f;
+            if (MT > 1 && !meet(ctx, group_bar, group_phase, lane)) break;
+        }
+        if (!(flags & kEmpty)) {
+            const uint8_t *const keys = smem + stage * 2 * L::kHalf, *const values = keys + L::kHalf;
+            // ---- logits of 16 tokens
+            float s[MT][2][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) s[mt][t][x] = 0.f;
+            uint32_t kw[2][kK];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(keys + chunk_at<D>(16 * warp + 8 * t + perm, c + 4 * h));
+                    kw[t][4 * h] = w.x; kw[t][4 * h + 1] = w.y; kw[t][4 * h + 2] = w.z; kw[t][4 * h + 3] = w.w;
+                }
+#pragma unroll
+            for (int k = 0; k < kK; ++k) {
+                uint32_t b[2][2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) { b[t][0] = to_f16x2(kw[t][k] & 0xffff); b[t][1] = to_f16x2(kw[t][k] >> 16); }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    uint4 a;
+                    if constexpr (MT == 1) a = make_uint4(qf[k][0], qf[k][1], qf[k][2], qf[k][3]);
+                    else a = query[(mt * kK + k) * 32 + lane];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) mma_f16(s[mt][t], a.x, a.y, a.z, a.w, b[t][0], b[t][1]);
+                }
+            }
+            // ---- values of the tokens a, b, a + 8, b + 8
+            uint32_t vw[4][D / 32];
+            const int tok[4] = {tok_a, tok_b, tok_a + 8, tok_b + 8};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int row = 16 * warp + tok[t];
+                if constexpr (D == 128) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(values + chunk_at<D>(row, perm));
+                    vw[t][0] = w.x; vw[t][1] = w.y; vw[t][2] = w.z; vw[t][3] = w.w;
+                } else {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(values + chunk_at<D>(row, n >> 1) + (n & 1) * 8);
+                    vw[t][0] = w.x; vw[t][1] = w.y;
+                }
+            }
+            const float ks = info.k_scale, vs = info.v_scale;
+            // ---- weights
+            bool grows = false;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) s[mt][t][x] *= rs[mt][x >> 1] * ks;
+            if (flags & kEdge) {
+                const int base = info.t0 + 16 * warp, lo = info.lo, hi = info.hi;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int at = base + tok[t];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (at < lo || at >= lim[mt][e]) s[mt][t >> 1][2 * e + (t & 1)] = -INFINITY;
+                    if (at < lo || at >= hi) {
+#pragma unroll
+                        for (int q = 0; q < D / 32; ++q) vw[t][q] = 0;
+                    }
+                }
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) grows |= s[mt][t][x] > m[mt][x >> 1] + kSlack;
+            if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float top = fmaxf(fmaxf(s[mt][0][2 * e], s[mt][0][2 * e + 1]), fmaxf(s[mt][1][2 * e], s[mt][1][2 * e + 1]));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                        top = fmaxf(top, m[mt][e]);
+                        if (top > m[mt][e]) {
+                            const float a = fast_exp2(m[mt][e] - top);       // (m = -inf: 0)
+                            m[mt][e] = top;
+                            l[mt][e] *= a;
+#pragma unroll
+                            for (int j = 0; j < kN; ++j) { o[mt][j][2 * e] *= a; o[mt][j][2 * e + 1] *= a; }
+                        }
+                    }
+            }
+            if (fabsf(vs) > unit) {
+                const float a = __fdiv_rn(unit, fabsf(vs));
+                unit = fabsf(vs);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int j = 0; j < kN; ++j)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) o[mt][j][x] *= a;
+            }
+            const float f = vs == unit ? 1.f : __fdiv_rn(vs, unit);
+            uint32_t pf[MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float ref = (m[mt][e] == -INFINITY ? 0.f : m[mt][e]) - kLift;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const float p0 = fast_exp2(s[mt][t][2 * e] - ref), p1 = fast_exp2(s[mt][t][2 * e + 1] - ref);
+                        l[mt][e] += p0 + p1;
+                        pf[mt][2 * t + e] = pack_f16x2(p0 * f, p1 * f);
+                        if (!(f == f))                                       // a scale that is NaN, for the rows that see the token
+                            pf[mt][2 * t + e] = (s[mt][t][2 * e] == -INFINITY ? 0u : 0x7fffu) | (s[mt][t][2 * e + 1] == -INFINITY ? 0u : 0x7fff0000u);
+                    }
+                }
+            // ---- a NaN value in a page where some rows do not see every token: products 0 * NaN must not reach the rows that do
+            // not see it.  Values without NaN go on; rows that see one get it by counting (weights 1 and 0) instead.
+            if (flags & kCausal) {
+                uint32_t nan = 0;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int q = 0; q < D / 32; ++q) nan |= ((vw[t][q] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                if (__any_sync(0xffffffffu, nan != 0)) {
+                    uint32_t nw[4][D / 32];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int q = 0; q < D / 32; ++q) {
+                            const uint32_t at = (((vw[t][q] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
+                            nw[t][q] = at * 0x38u;                      // 1.0
+                            vw[t][q] &= ~(at * 0xffu);
+                        }
+                    const int base = info.t0 + 16 * warp;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        uint32_t sees[4];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int t = 0; t < 2; ++t)
+                                sees[2 * t + e] = (base + tok[2 * t] < lim[mt][e] ? 0x3c00u : 0u) | (base + tok[2 * t + 1] < lim[mt][e] ? 0x3c000000u : 0u);
+#pragma unroll
+                        for (int j = 0; j < kN; ++j) {
+                            const uint32_t sel = (j & 2) ? 0x7362 : 0x5140;
+                            const uint32_t x = __byte_perm(nw[0][j / 4], nw[1][j / 4], sel), y = __byte_perm(nw[2][j / 4], nw[3][j / 4], sel);
+                            float count[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_f16(count, sees[0], sees[1], sees[2], sees[3], to_f16x2((j & 1) ? x >> 16 : x & 0xffff), to_f16x2((j & 1) ? y >> 16 : y & 0xffff));
+#pragma unroll
+                            for (int x2 = 0; x2 < 4; ++x2)
+                                if (count[x2] > 0.f) o[mt][j][x2] = NAN;
+                        }
+                    }
+                }
+            }
+            // ---- outputs
+#pragma unroll
+            for (int q = 0; q < D / 32; ++q)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t sel = half ? 0x7362 : 0x5140;
+                    const uint32_t x = __byte_perm(vw[0][q], vw[1][q], sel), y = __byte_perm(vw[2][q], vw[3][q], sel);
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const int j = 4 * q + 2 * half + z;
+                        const uint32_t b0 = to_f16x2(z ? x >> 16 : x & 0xffff), b1 = to_f16x2(z ? y >> 16 : y & 0xffff);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) mma_f16(o[mt][j], pf[mt][0], pf[mt][1], pf[mt][2], pf[mt][3], b0, b1);
+                    }
+                }
+        }
+        if (flags & (kLast | kEmpty)) {
+            // ---- the four warps' parts of the item
+            const int m0 = info.m0, pairs = info.pairs, row0 = info.row0, head = info.head, slot = info.slot;
+            float *const stat_l = stat_m + kConsumers * L::kRows;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * stage);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    l[mt][e] += __shfl_xor_sync(0xffffffffu, l[mt][e], 1);
+                    l[mt][e] += __shfl_xor_sync(0xffffffffu, l[mt][e], 2);
+                    if (c == 0) {
+                        stat_m[warp * L::kRows + mt * 16 + n + 8 * e] = m[mt][e];
+                        stat_l[warp * L::kRows + mt * 16 + n + 8 * e] = l[mt][e];
+                    }
+                }
+            if (!meet(ctx, group_bar, group_phase, lane)) break;
+            bool ok = true;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = mt * 16 + n + 8 * e;
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < kConsumers; ++w) top = fmaxf(top, stat_m[w * L::kRows + r]);
+                    const float a = fast_exp2(m[mt][e] - (top == -INFINITY ? 0.f : top));
+                    float *const to = merge + (warp * 16 + n + 8 * e) * L::kPad;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        // columns 2c and 2c + 1 of all MMAs: successive dimensions
+                        const int d = D == 128 ? 64 * half + 16 * c : 16 * c + 8 * half;
+#pragma unroll
+                        for (int j = 0; j < kN; j += 4)
+                            *reinterpret_cast<float4 *>(to + d + j) = make_float4(o[mt][j][2 * e + half] * a, o[mt][j + 1][2 * e + half] * a,
+                                                                                  o[mt][j + 2][2 * e + half] * a, o[mt][j + 3][2 * e + half] * a);
+                    }
+                }
+                if (!(ok = meet(ctx, group_bar, group_phase, lane))) break;
+                const int tid = warp * 32 + lane, r16 = tid >> 3, r = mt * 16 + r16, mm = m0 + r;
+                if (mm < pairs) {
+                    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kConsumers; ++w) top = fmaxf(top, stat_m[w * L::kRows + r]);
+                    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                    for (int w = 0; w < kConsumers; ++w) sum += stat_l[w * L::kRows + r] * fast_exp2(stat_m[w * L::kRows + r] - ref);
+                    const float scale = sum == 0.f ? 0.f : unit / sum;
+                    const float lse2 = sum == 0.f ? -INFINITY : ref + __log2f(sum) - kLift;
+                    const int row = mm / p.group, g = head * p.group + mm - row * p.group;
+#pragma unroll
+                    for (int q = 0; q < D / 32; ++q) {
+                        const int d = 4 * ((tid & 7) + 8 * q);
+                        float4 v = *reinterpret_cast<const float4 *>(merge + r16 * L::kPad + d);
+#pragma unroll
+                        for (int w = 1; w < kConsumers; ++w) {
+                            const float4 x = *reinterpret_cast<const float4 *>(merge + (w * 16 + r16) * L::kPad + d);
+                            v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                        }
+                        v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
+                        if (slot < 0) store4(p, (row0 + row) * p.out_row + g * p.out_head + d, v);
+                        else *reinterpret_cast<float4 *>(p.part_out + ((int64_t)slot * L::kRows + r) * D + d) = v;
+                    }
+                    if ((tid & 7) == 0) {
+                        if (slot < 0) p.lse[(row0 + row) * p.lse_row + g] = lse2 * kLn2;
+                        else p.part_lse[slot * L::kRows + r] = lse2;
+                    }
+                }
+                if (MT > 1 && mt + 1 < MT && !(ok = meet(ctx, group_bar, group_phase, lane))) break;
+            }
+            if (!ok) break;
+            stat_m = reinterpret_cast<float *>(smem + L::kStats) + (stat_m == reinterpret_cast<float *>(smem + L::kStats) ? 2 * kConsumers * L::kRows : 0);
+        } else {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * stage);
+        }
+        if (++stage == L::kStages) { stage = 0; phase ^= 1; }
+    }
+}
+
+template <int D, int MT>
+__global__ void __launch_bounds__(kThreads, 2)
+kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using L = Layout<D, MT>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint32_t abort_flag;
+    uint8_t *const smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    const uint32_t bars = smem_u32(smem + L::kBars);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, worker = blockIdx.x;
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int s = 0; s < L::kStages; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (L::kStages + s), kConsumers); }
+        mbar_init(bars + 16 * L::kStages, kConsumers);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (blockIdx.x == 0 && threadIdx.x < 4) p.status[threadIdx.x] = 0;
+    const Share share = plan<L::kRows>(p, worker);      // (its barriers publish the mbarriers too)
+    const Ctx ctx = {&abort_flag, p.status};
+    if (warp == kConsumers) produce<D, MT>(p, share, &k_map, &v_map, smem, bars, ctx, worker, lane);
+    else consume<D, MT>(p, smem, bars, ctx, warp, lane);
+}
+
+// Pieces of the cut items, [piece][row][D] with their base-2 lse: out = sum_j 2^(lse_j - lse) out_j.  Block (worker, group of four
+// rows), a warp per row; the pieces of an item lie in the last slot of its first worker and the first slots of the following ones.
+template <int D, int kRows>
+__global__ void __launch_bounds__(128)
+kv8_combine_kernel(const __grid_constant__ AttnParams p) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int worker = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int4 cut = p.cut[worker];
+    if (cut.z == 0) return;
+    const Request req = request(p, cut.x);
+    const int tiles = (req.pairs + kRows - 1) / kRows, head = cut.y / tiles;
+    const int r = blockIdx.y * 4 + warp, mm = (cut.y % tiles) * kRows + r;
+    if (mm >= req.pairs) return;
+    auto slot = [&](int j) { return j == 0 ? 2 * worker + 1 : 2 * (worker + j); };
+    float top = -INFINITY;
+    for (int j = lane; j < cut.z; j += 32) top = fmaxf(top, p.part_lse[slot(j) * kRows + r]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float ref = top == -INFINITY ? 0.f : top;
+    constexpr int kPer = D / 32;
+    float acc[kPer] = {}, sum = 0.f;
+    for (int j0 = 0; j0 < cut.z; j0 += 8) {
+        float w[8], v[8][kPer];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bool there = j0 + k < cut.z;
+            const int64_t at = (int64_t)slot(there ? j0 + k : 0) * kRows + r;
+            w[k] = there ? fast_exp2(p.part_lse[at] - ref) : 0.f;
+            if constexpr (kPer == 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(p.part_out + at * D + lane * 4);
+                v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
+            } else {
+                const float2 x = *reinterpret_cast<const float2 *>(p.part_out + at * D + lane * 2);
+                v[k][0] = x.x; v[k][1] = x.y;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (j0 + k >= cut.z) break;
+            sum += w[k];
+#pragma unroll
+            for (int x = 0; x < kPer; ++x) acc[x] += w[k] * v[k][x];
+        }
+    }
+    const float scale = sum == 0.f ? 0.f : 1.f / sum;
+    const int row = mm / p.group, g = head * p.group + mm - row * p.group;
+    const int64_t at = (int64_t)(req.row0 + row) * p.out_row + g * p.out_head + lane * kPer;
+    if constexpr (kPer == 4) {
+        store4(p, at, make_float4(acc[0] * scale, acc[1] * scale, acc[2] * scale, acc[3] * scale));
+    } else if (p.out_f32) {
+        *reinterpret_cast<float2 *>(static_cast<float *>(p.out) + at) = make_float2(acc[0] * scale, acc[1] * scale);
+    } else {
+        *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.out) + at) =
+            p.q_bf16 ? pack_bf16x2(acc[0] * scale, acc[1] * scale) : pack_f16x2(acc[0] * scale, acc[1] * scale);
+    }
+    if (lane == 0) p.lse[(int64_t)(req.row0 + row) * p.lse_row + g] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+}
+
+bool make_pool_map(CUtensorMap *map, const splash_kv8_cache &c, const void *pool, int64_t page_stride, int64_t head_stride) {
+    EncodeTiledFn fn = encode_tiled();
+    if (!fn) { set_error("cuTensorMapEncodeTiled is not available"); return false; }
+    const uint64_t D = (uint64_t)c.head_dim;
+    cuuint64_t dims[4] = {D, 64, (cuuint64_t)c.num_kv_heads, (cuuint64_t)c.num_pages};
+    // (strides of dimensions of one element are the caller's own business)
+    cuuint64_t strides[3] = {D, (cuuint64_t)(c.num_kv_heads > 1 ? head_stride : 64 * D), (cuuint64_t)(c.num_pages > 1 ? page_stride : 64 * D)};
+    cuuint32_t box[4] = {(cuuint32_t)D, 64, 1, 1}, step[4] = {1, 1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(pool), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) set_error("cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return r == CUDA_SUCCESS;
+}
+
+template <int D, int MT>
+cudaError_t launch_decode(const AttnParams &p, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
+    using L = Layout<D, MT>;
+    static DeviceOnce once;
+    cudaError_t e = once.run([] {
+        return cudaFuncSetAttribute(kv8_decode_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    });
+    if (e != cudaSuccess) return e;
+    e = launch_dependent(kv8_decode_kernel<D, MT>, dim3(p.workers), dim3(kThreads), L::kBytes, stream, p, k_map, v_map);
+    count_launch();
+    if (e != cudaSuccess || p.whole) return e;
+    e = launch_dependent(kv8_combine_kernel<D, L::kRows>, dim3(p.workers, L::kRows / 4), dim3(128), 0, stream, p);
+    count_launch();
+    return e;
+}
+
+}  // namespace
+
+int kv8_decode_workers(int sm_count) { return 2 * sm_count; }
+
+bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v_map) {
+    return make_pool_map(k_map, c, c.k_pool, c.k_page_stride, c.k_head_stride) && make_pool_map(v_map, c, c.v_pool, c.v_page_stride, c.v_head_stride);
+}
+
+cudaError_t launch_kv8_decode(const AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
+    if (D == 128) return rows <= 16 ? launch_decode<128, 1>(p, k_map, v_map, stream) : launch_decode<128, 2>(p, k_map, v_map, stream);
+    return rows <= 16 ? launch_decode<64, 1>(p, k_map, v_map, stream) : launch_decode<64, 2>(p, k_map, v_map, stream);
+}
+
+}  // namespace splash

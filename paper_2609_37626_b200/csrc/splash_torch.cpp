@@ -8,6 +8,8 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -488,6 +490,205 @@ PyObject *dop_unpack_rows(PyObject *, PyObject *const *args, Py_ssize_t nargs, P
     END_HANDLE_TH_ERRORS
 }
 
+// ---- keys and values in 8 bits ----------------------------------------------------------------------------------------
+
+// All of them on the GPU, on one device (None aside).
+bool on_one_gpu(std::initializer_list<const at::Tensor *> tensors) {
+    const at::Tensor *first = nullptr;
+    for (const at::Tensor *t : tensors) {
+        if (t == nullptr) continue;
+        if (!t->is_cuda()) { PyErr_SetString(PyExc_AssertionError, "the tensors must be on the GPU"); return false; }
+        if (first == nullptr) first = t;
+        if (t->device() != first->device()) { PyErr_SetString(PyExc_AssertionError, "the tensors must be on one device"); return false; }
+    }
+    return true;
+}
+
+bool dense_int(const at::Tensor *t, int64_t n) {
+    return t == nullptr || (t->scalar_type() == at::kInt && t->dim() == 1 && (n < 0 || t->numel() == n) && (t->numel() < 2 || t->stride(0) == 1));
+}
+
+// The stream of a call on `device`: the argument's, or the current one of that device.
+bool stream_on(PyObject *o, c10::DeviceIndex device, void *&stream) {
+    if (!given(o)) { stream = c10::cuda::getCurrentCUDAStream(device).stream(); return true; }
+    return stream_of(o, stream);
+}
+
+const char *const kSlotNames[] = {"block_table", "seq_lens", "new_lens", "free_pages", "free_begin", "num_slots", "slot_map", "positions", "q_start",
+                                  "new_seq_lens", "counts", "stream"};
+Signature sig_slots{"splash_kv_slots", 6, 6, 12, kSlotNames, nullptr};
+
+PyObject *kv_slots(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+    HANDLE_TH_ERRORS
+    PyObject *v[12];
+    if (!parse(sig_slots, args, nargs, kwnames, v)) return nullptr;
+    const at::Tensor *table, *lens, *more, *free_pages, *begin, *given_out[5];
+    if (!(table = tensor(v[0], "block_table")) || !(lens = tensor(v[1], "seq_lens")) || !(more = tensor(v[2], "new_lens")) ||
+        !(free_pages = tensor(v[3], "free_pages")) || !(begin = tensor(v[4], "free_begin")))
+        return nullptr;
+    int64_t places;
+    if (!integer(v[5], 0, places)) return nullptr;
+    for (int k = 0; k < 5; ++k)
+        if (!maybe_tensor(v[6 + k], kSlotNames[6 + k], given_out[k])) return nullptr;
+    const int64_t B = lens->numel();
+    SPLASH_ASSERT(table->dim() == 2 && table->scalar_type() == at::kInt && table->size(0) == B && (table->numel() == 0 || table->size(1) < 2 || table->stride(1) == 1));
+    SPLASH_ASSERT(dense_int(lens, B) && dense_int(more, B) && dense_int(free_pages, -1) && dense_int(begin, 1));
+    SPLASH_ASSERT(places >= 0);
+    if (!on_one_gpu({table, lens, more, free_pages, begin, given_out[0], given_out[1], given_out[2], given_out[3], given_out[4]})) return nullptr;
+    const c10::cuda::CUDAGuard guard(table->device());
+    const int64_t sizes[5] = {places, places, B + 1, B, 4};
+    at::Tensor out[5];
+    for (int k = 0; k < 5; ++k) {
+        if (given_out[k] == nullptr) { out[k] = new_tensor({sizes[k]}, k == 0 ? at::kLong : at::kInt, *table); continue; }
+        out[k] = *given_out[k];
+        SPLASH_ASSERT(out[k].dim() == 1 && out[k].numel() == sizes[k] && out[k].is_contiguous() && out[k].scalar_type() == (k == 0 ? at::kLong : at::kInt));
+    }
+    void *stream;
+    if (!stream_on(v[11], table->device().index(), stream)) return nullptr;
+    void *const table_at = table->data_ptr(), *const slot_at = out[0].data_ptr(), *const pos_at = out[1].data_ptr(), *const start_at = out[2].data_ptr(),
+               *const after_at = out[3].data_ptr(), *const counts_at = out[4].data_ptr();
+    const void *const lens_at = lens->data_ptr(), *const more_at = more->data_ptr(), *const free_at = free_pages->data_ptr(), *const begin_at = begin->data_ptr();
+    const int64_t num_free = free_pages->numel(), stride = table->stride(0), width = table->size(1);
+    SPLASH_ASSERT(width <= INT32_MAX && B <= INT32_MAX);
+    const int rc = without_gil([&] {
+        return splash_kv_slots((int32_t)B, (const int32_t *)lens_at, (const int32_t *)more_at, (const int32_t *)free_at, num_free, (const int32_t *)begin_at,
+                               (int32_t *)table_at, stride, (int32_t)width, places, (int64_t *)slot_at, (int32_t *)pos_at, (int32_t *)start_at,
+                               (int32_t *)after_at, (int32_t *)counts_at, stream);
+    });
+    if (rc != SPLASH_OK) return raise_status(rc);
+    PyObject *result = PyTuple_New(5);
+    for (int k = 0; result && k < 5; ++k) {
+        PyObject *o = given_out[k] ? Py_NewRef(v[6 + k]) : THPVariable_Wrap(out[k]);
+        if (!o) { Py_DECREF(result); return nullptr; }
+        PyTuple_SET_ITEM(result, k, o);
+    }
+    return result;
+    END_HANDLE_TH_ERRORS
+}
+
+// The cache's struct from its tensors [P][heads][64][D] and [P][heads]; false with an AssertionError set when they do not fit together.
+bool fill_cache(splash_kv8_cache &c, const at::Tensor &k, const at::Tensor &v, const at::Tensor &ks, const at::Tensor &vs) {
+    auto fail = [](const char *what) { PyErr_SetString(PyExc_AssertionError, what); return false; };
+    for (const at::Tensor *t : {&k, &v}) {
+        if (t->scalar_type() != at::kByte && t->scalar_type() != at::kFloat8_e4m3fn) return fail("pools must be uint8 or float8_e4m3fn");
+        if (t->dim() != 4 || t->size(2) != 64) return fail("pools must be [pages][heads][64][head_dim]");
+        if (t->stride(3) != 1 || t->stride(2) != t->size(3)) return fail("the rows of a (page, head) must be dense");
+    }
+    if (k.sizes() != v.sizes()) return fail("k_pool and v_pool must have one shape");
+    for (const at::Tensor *t : {&ks, &vs}) {
+        if (t->scalar_type() != at::kFloat || t->dim() != 2 || t->size(0) != k.size(0) || t->size(1) != k.size(1)) return fail("scales must be fp32 [pages][heads]");
+        if (t->size(1) > 1 && t->stride(1) != 1) return fail("scales must be dense along the heads");
+    }
+    if (k.size(0) > INT32_MAX || k.size(1) > INT32_MAX || k.size(3) > INT32_MAX) return fail("a dimension of the pools is too large");
+    c = splash_kv8_cache{};
+    c.struct_size = sizeof c;
+    c.num_pages = (int32_t)k.size(0); c.num_kv_heads = (int32_t)k.size(1); c.head_dim = (int32_t)k.size(3); c.page_size = 64;
+    c.k_pool = k.data_ptr(); c.v_pool = v.data_ptr();
+    c.k_scales = (float *)ks.data_ptr(); c.v_scales = (float *)vs.data_ptr();
+    c.k_page_stride = k.stride(0); c.k_head_stride = k.stride(1); c.v_page_stride = v.stride(0); c.v_head_stride = v.stride(1);
+    c.k_scale_stride = ks.stride(0); c.v_scale_stride = vs.stride(0);
+    return true;
+}
+
+int kv8_dtype(const at::Tensor &t) {
+    return t.scalar_type() == at::kBFloat16 ? SPLASH_DTYPE_BF16 : t.scalar_type() == at::kHalf ? SPLASH_DTYPE_FP16 : t.scalar_type() == at::kFloat ? SPLASH_DTYPE_FP32 : -1;
+}
+
+const char *const kAppendNames[] = {"k", "v", "slot_map", "k_pool", "v_pool", "k_scales", "v_scales", "stream"};
+Signature sig_append{"splash_kv8_append", 7, 7, 8, kAppendNames, nullptr};
+
+PyObject *kv8_append(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+    HANDLE_TH_ERRORS
+    PyObject *o[8];
+    if (!parse(sig_append, args, nargs, kwnames, o)) return nullptr;
+    const at::Tensor *t[7];
+    for (int i = 0; i < 7; ++i)
+        if (!(t[i] = tensor(o[i], kAppendNames[i]))) return nullptr;
+    const at::Tensor &k = *t[0], &v = *t[1], &slots = *t[2];
+    splash_kv8_cache cache;
+    if (!fill_cache(cache, *t[3], *t[4], *t[5], *t[6])) return nullptr;
+    SPLASH_ASSERT(k.dim() == 3 && k.sizes() == v.sizes() && k.scalar_type() == v.scalar_type());
+    SPLASH_ASSERT(k.size(1) == cache.num_kv_heads && k.size(2) == cache.head_dim);
+    SPLASH_ASSERT(k.numel() == 0 || (k.stride(2) == 1 && v.stride(2) == 1));
+    SPLASH_ASSERT(slots.scalar_type() == at::kLong && slots.dim() == 1 && slots.numel() == k.size(0) && (slots.numel() < 2 || slots.stride(0) == 1));
+    if (!on_one_gpu({t[0], t[1], t[2], t[3], t[4], t[5], t[6]})) return nullptr;
+    const c10::cuda::CUDAGuard guard(k.device());
+    void *stream;
+    if (!stream_on(o[7], k.device().index(), stream)) return nullptr;
+    const void *const k_at = k.data_ptr(), *const v_at = v.data_ptr(), *const slots_at = slots.data_ptr();
+    const int64_t n = k.size(0), kr = k.stride(0), kh = k.stride(1), vr = v.stride(0), vh = v.stride(1);
+    const int dtype = kv8_dtype(k);
+    const int rc = without_gil([&] { return splash_kv8_append(&cache, dtype, n, k_at, kr, kh, v_at, vr, vh, (const int64_t *)slots_at, stream); });
+    if (rc != SPLASH_OK) return raise_status(rc);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+const char *const kAttendNames[] = {"q", "k_pool", "v_pool", "k_scales", "v_scales", "block_table", "seq_lens", "softmax_scale", "q_start", "max_q_rows",
+                                    "kv_begin", "kv_end", "out", "lse", "workspace", "stream"};
+Signature sig_attend{"splash_kv8_attention", 7, 8, 16, kAttendNames, nullptr};
+
+PyObject *kv8_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+    HANDLE_TH_ERRORS
+    PyObject *o[16];
+    if (!parse(sig_attend, args, nargs, kwnames, o)) return nullptr;
+    const at::Tensor *t[7], *start, *begin, *end, *ws, *given_out, *given_lse;
+    for (int i = 0; i < 7; ++i)
+        if (!(t[i] = tensor(o[i], kAttendNames[i]))) return nullptr;
+    const double scale = PyFloat_AsDouble(o[7]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    int64_t most;
+    if (!maybe_tensor(o[8], "q_start", start) || !integer(o[9], 1, most) || !maybe_tensor(o[10], "kv_begin", begin) || !maybe_tensor(o[11], "kv_end", end) ||
+        !maybe_tensor(o[12], "out", given_out) || !maybe_tensor(o[13], "lse", given_lse) || !maybe_tensor(o[14], "workspace", ws))
+        return nullptr;
+    const at::Tensor &q = *t[0], &table = *t[5], &lens = *t[6];
+    splash_kv8_cache cache;
+    if (!fill_cache(cache, *t[1], *t[2], *t[3], *t[4])) return nullptr;
+    const int64_t B = lens.numel();
+    SPLASH_ASSERT(q.dim() == 3 && q.size(2) == cache.head_dim && (q.numel() == 0 || q.stride(2) == 1));
+    SPLASH_ASSERT(table.dim() == 2 && table.scalar_type() == at::kInt && table.size(0) == B && (table.numel() == 0 || table.size(1) < 2 || table.stride(1) == 1));
+    SPLASH_ASSERT(dense_int(&lens, B) && dense_int(start, B + 1) && dense_int(begin, B) && dense_int(end, B));
+    SPLASH_ASSERT(B <= INT32_MAX && table.size(1) <= INT32_MAX && q.size(1) <= INT32_MAX && most >= 1 && most <= INT32_MAX);
+    if (!on_one_gpu({t[0], t[1], t[2], t[3], t[4], t[5], t[6], start, begin, end, ws, given_out, given_lse})) return nullptr;
+    const c10::cuda::CUDAGuard guard(q.device());
+    void *stream;
+    if (!stream_on(o[15], q.device().index(), stream)) return nullptr;
+    at::Tensor out, lse;
+    if (given_out) out = *given_out; else out = new_tensor({q.size(0), q.size(1), q.size(2)}, q.scalar_type(), q);
+    if (given_lse) lse = *given_lse; else lse = new_tensor({q.size(0), q.size(1)}, at::kFloat, q);
+    SPLASH_ASSERT(out.sizes() == q.sizes() && (out.numel() == 0 || out.stride(2) == 1));
+    SPLASH_ASSERT(lse.scalar_type() == at::kFloat && lse.dim() == 2 && lse.size(0) == q.size(0) && lse.size(1) == q.size(1) && (lse.numel() == 0 || lse.size(1) < 2 || lse.stride(1) == 1));
+    splash_kv8_query s = {};
+    s.struct_size = sizeof s;
+    s.num_requests = (int32_t)B; s.num_rows = q.size(0); s.num_heads = (int32_t)q.size(1); s.max_q_rows = (int32_t)most;
+    s.dtype = kv8_dtype(q); s.out_dtype = kv8_dtype(out);
+    s.q_row_stride = q.stride(0); s.q_head_stride = q.stride(1); s.out_row_stride = out.stride(0); s.out_head_stride = out.stride(1);
+    s.lse_row_stride = lse.stride(0); s.block_table_stride = table.stride(0); s.table_width = (int32_t)table.size(1);
+    s.softmax_scale = (float)scale;
+    // Scratch for this call alone, given back to the allocator behind it: calls on two streams, or in two captured graphs, share none.
+    at::Tensor scratch;
+    if (ws == nullptr) {
+        const size_t need = splash_kv8_attention_workspace_bytes(&cache, &s);
+        if (need == 0) return raise_status(splash_kv8_attention(&cache, &s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, stream));
+        scratch = new_tensor({(int64_t)need}, at::kByte, q);
+        if (given(o[15])) c10::cuda::CUDACachingAllocator::recordStream(scratch.storage().data_ptr(), c10::cuda::getStreamFromExternal((cudaStream_t)stream, q.device().index()));
+    } else {
+        scratch = *ws;
+        SPLASH_ASSERT(scratch.is_contiguous());
+    }
+    const void *const q_at = q.data_ptr(), *const table_at = table.data_ptr(), *const lens_at = lens.data_ptr(), *const start_at = ptr(start),
+                     *const begin_at = ptr(begin), *const end_at = ptr(end);
+    void *const out_at = out.data_ptr(), *const lse_at = lse.data_ptr(), *const ws_at = scratch.data_ptr();
+    const size_t ws_bytes = (size_t)scratch.numel() * scratch.element_size();
+    const int rc = without_gil([&] {
+        return splash_kv8_attention(&cache, &s, q_at, (const int32_t *)table_at, (const int32_t *)lens_at, (const int32_t *)start_at, (const int32_t *)begin_at,
+                                    (const int32_t *)end_at, out_at, (float *)lse_at, ws_at, ws_bytes, stream);
+    });
+    if (rc != SPLASH_OK) return raise_status(rc);
+    return pair_of(o[12], out, o[13], lse);
+    END_HANDLE_TH_ERRORS
+}
+
 // ---- module -----------------------------------------------------------------------------------------------------------
 
 PyObject *set_error_class(PyObject *, PyObject *cls) {
@@ -550,6 +751,25 @@ PyMethodDef kMethods[] = {
     {"splash_dop_unpack_rows", FAST(dop_unpack_rows), METH_FASTCALL | METH_KEYWORDS,
      "splash_dop_unpack_rows(recv, send_row, out, stream=None)\n--\n\n"
      "out[send_row[p]] = recv[p]; recv [n][...] contiguous, out [N][...] with contiguous rows.\n"},
+    {"splash_kv_slots", FAST(kv_slots), METH_FASTCALL | METH_KEYWORDS,
+     "splash_kv_slots(block_table, seq_lens, new_lens, free_pages, free_begin, num_slots, *, slot_map=None, positions=None, "
+     "q_start=None, new_seq_lens=None, counts=None, stream=None)\n--\n\n"
+     "Places of a step's new tokens, from the lengths on the device; see splash_kv_slots in include/splash_mla.h.\n\n"
+     "block_table [B][width] int32 gets the ids of new pages, in place; seq_lens, new_lens [B], free_pages [F],\n"
+     "free_begin [1] int32.  Returns (slot_map [num_slots] int64, positions [num_slots], q_start [B + 1],\n"
+     "new_seq_lens [B], counts [4] int32: places asked for, pages taken, requests refused, the next free_begin).\n"},
+    {"splash_kv8_append", FAST(kv8_append), METH_FASTCALL | METH_KEYWORDS,
+     "splash_kv8_append(k, v, slot_map, k_pool, v_pool, k_scales, v_scales, *, stream=None)\n--\n\n"
+     "Write keys and values into an e4m3 cache, in place; see splash_kv8_append in include/splash_mla.h.\n\n"
+     "k, v [N][heads][D] bf16 or fp16 (D 64 or 128, any row and head strides); slot_map [N] int64, negative: skipped;\n"
+     "pools [P][heads][64][D] uint8 or float8_e4m3fn, scales [P][heads] fp32.\n"},
+    {"splash_kv8_attention", FAST(kv8_attention), METH_FASTCALL | METH_KEYWORDS,
+     "splash_kv8_attention(q, k_pool, v_pool, k_scales, v_scales, block_table, seq_lens, *, softmax_scale, q_start=None, "
+     "max_q_rows=1, kv_begin=None, kv_end=None, out=None, lse=None, workspace=None, stream=None)\n--\n\n"
+     "Causal attention of each request's newest rows over an e4m3 cache; see splash_kv8_attention in include/splash_mla.h.\n\n"
+     "q [T][H][D] bf16 or fp16, rows q_start[i] .. q_start[i + 1] - 1 belong to request i (None: row i), at most max_q_rows each;\n"
+     "pools and scales as for splash_kv8_append, H a multiple of their heads; block_table [B][width], seq_lens, kv_begin, kv_end [B] int32.\n"
+     "Returns (out [T][H][D] of q's type, or the given fp32 tensor; lse [T][H] fp32).\n"},
     {"set_error_class", set_error_class, METH_O, "The exception class of a call that did not succeed."},
     {"cached_workspace", cached, METH_VARARGS, "The scratch buffer that calls without one share on a device, or None."},
     {nullptr, nullptr, 0, nullptr}};
@@ -560,6 +780,6 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_splash_torch", "Native entry poi
 }  // namespace
 
 PyMODINIT_FUNC PyInit__splash_torch() {
-    for (Signature *s : {&sig_decode, &sig_sparse, &sig_merge, &sig_migrate, &sig_migrate_static, &sig_pack, &sig_swap, &sig_unpack}) intern(*s);
+    for (Signature *s : {&sig_decode, &sig_sparse, &sig_merge, &sig_migrate, &sig_migrate_static, &sig_pack, &sig_swap, &sig_unpack, &sig_slots, &sig_append, &sig_attend}) intern(*s);
     return PyModule_Create(&kModule);
 }
