@@ -10,11 +10,9 @@ namespace kv8 {
 
 constexpr int kMinExp = -100;     // scales that an append writes are at least 2^-100 (and their reciprocals are finite)
 
-// two e4m3 codes -> two fp16 values (every e4m3 value is an fp16 value), the lower byte in the lower half
-__device__ __forceinline__ uint32_t to_f16x2(uint32_t codes /* low 16 bits */) {
-    uint32_t r;
-    asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(codes));
-    return r;
+// four e4m3 codes -> fp16 values (every e4m3 value is an fp16 value), the codes' order kept
+__device__ __forceinline__ void to_f16x4(uint32_t codes, uint32_t &lo, uint32_t &hi) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 // two fp32 values -> two e4m3 codes, nearest even, above 448 -> 448, NaN -> NaN
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
@@ -41,7 +39,8 @@ struct AttnParams {
     float scale_log2;                 // softmax scale times log2 e
     // workspace
     int32_t *status;                  // 16 ints
-    int4 *cut;                        // [workers]: {request, part of it, pieces, 0} of the cut item whose first piece the worker has; pieces = 0: none
+    int4 *cut;                        // [workers][2]: {pieces, first query row, pairs, first pair of the tile}, {key head, 0, 0, 0} of the cut item
+                                      // whose first piece the worker has; pieces = 0: none
     float *part_lse;                  // [2 workers][rows], base 2
     float *part_out;                  // [2 workers][rows][D]
 };

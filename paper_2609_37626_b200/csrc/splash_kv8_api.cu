@@ -13,7 +13,7 @@ cudaError_t launch_kv_slots(int32_t B, const int32_t *seq_lens, const int32_t *n
                             cudaStream_t stream);
 cudaError_t launch_kv8_append(const splash_kv8_cache &cache, int32_t dtype, int64_t rows, const void *k, int64_t k_row, int64_t k_head, const void *v,
                               int64_t v_row, int64_t v_head, const int64_t *slot_map, int sm_count, cudaStream_t stream);
-int kv8_decode_workers(int sm_count);
+void kv8_decode_shape(int64_t pairs, int head_dim, int sm_count, int *rows, int *workers);
 bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v_map);
 cudaError_t launch_kv8_decode(const kv8::AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream);
 
@@ -87,16 +87,16 @@ View carve(void *base, int workers, int rows, int D) {
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return b + here; };
     View v;
     v.status = reinterpret_cast<int32_t *>(take(64));
-    v.cut = reinterpret_cast<int4 *>(take((size_t)workers * sizeof(int4)));
+    v.cut = reinterpret_cast<int4 *>(take((size_t)workers * 2 * sizeof(int4)));
     v.lse = reinterpret_cast<float *>(take((size_t)2 * workers * rows * 4));
     v.out = reinterpret_cast<float *>(take((size_t)2 * workers * rows * D * 4));
     v.bytes = at;
     return v;
 }
 
-// rows of a tile of (row, head) pairs
-int tile_rows(const splash_kv8_cache *c, const splash_kv8_query *s) {
-    return (int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads) <= 16 ? 16 : 32;
+View carve(void *base, const splash_kv8_cache *c, const splash_kv8_query *s, int sms, int &rows, int &workers) {
+    kv8_decode_shape((int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads), c->head_dim, sms, &rows, &workers);
+    return carve(base, workers, rows, c->head_dim);
 }
 
 }  // namespace
@@ -164,7 +164,8 @@ size_t splash_kv8_attention_workspace_bytes(const splash_kv8_cache *cache, const
     if (check_cache(cache) != SPLASH_OK || check_query(cache, query) != SPLASH_OK) return 0;
     int sms = 0;
     if (usable_device(sms) != SPLASH_OK) return 0;
-    return carve(nullptr, kv8_decode_workers(sms), tile_rows(cache, query), cache->head_dim).bytes;
+    int rows, workers;
+    return carve(nullptr, cache, query, sms, rows, workers).bytes;
 }
 
 int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *query, const void *q, const int32_t *block_table,
@@ -183,8 +184,8 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
     int sms = 0;
     rc = usable_device(sms);
     if (rc != SPLASH_OK) return rc;
-    const int rows = tile_rows(cache, query), workers = kv8_decode_workers(sms);
-    const View v = carve(workspace, workers, rows, cache->head_dim);
+    int rows, workers;
+    const View v = carve(workspace, cache, query, sms, rows, workers);
     if (workspace_bytes < v.bytes) {
         set_error("workspace has %zu bytes, %zu needed", workspace_bytes, v.bytes);
         return SPLASH_INVALID_ARG;

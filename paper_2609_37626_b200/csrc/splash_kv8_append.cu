@@ -179,11 +179,11 @@ kv8_append_kernel(const AppendParams p) {
             uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                uint32_t out = 0;
+                uint32_t out = 0, h2[2];
+                to_f16x4(w[q], h2[0], h2[1]);
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const uint32_t h2 = to_f16x2(w[q] >> (16 * half) & 0xffff);
-                    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+                    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h2[half]));
                     out |= to_e4m3x2(v.x * from * unit, v.y * from * unit) << (16 * half);
                 }
                 w[q] = out;

@@ -19,6 +19,8 @@
 //     MMAs; values: tokens c, c + 4, c + 8, c + 12 and the chunk perm(n), bytes of two tokens interleaved.
 // mma.sync and not tcgen05: with at most 32 rows the MMAs take a fifth of the time that the bytes take, and the 8-bit
 // operands would have to be widened into shared memory first, twice the bytes over the path that is next in line.
+#include <type_traits>
+
 #include "splash_kv8.cuh"
 #include "splash_umma.cuh"
 
@@ -34,6 +36,7 @@ constexpr int kThreads = 32 * (kConsumers + 1);
 constexpr int kOverhead = 2;                        // cost of an item beside its pages, in pages
 constexpr int kMinUnits = 2;                        // least cost of a worker's share
 constexpr float kLift = 7.f, kSlack = 8.f;          // weights are kept below 2^(kLift + kSlack) = 2^15
+constexpr float kUnset = -1e38f;                    // reference of a row that has seen no token: any logit is far above it
 
 enum { kFirst = 1, kLast = 2, kEmpty = 4, kEnd = 8, kEdge = 16, kCausal = 32 };
 
@@ -46,23 +49,31 @@ struct alignas(16) PageInfo {
     int pad2[2];
 };
 
-template <int D, int MT>
+// NT: tiles of eight rows
+template <int D, int NT>
 struct Layout {
-    static constexpr int kRows = 16 * MT;
-    static constexpr int kStages = D == 128 ? 4 : 8;
+    static constexpr int kRows = 8 * NT;
+    static constexpr int kCtas = 3;                                        // blocks of an SM
+    static constexpr bool kQueryShared = NT > 1;                           // queries as MMA operands in shared memory, or in registers
+    static constexpr int kStages = D == 128 ? 3 : 6;
     static constexpr int kHalf = 64 * D;                                   // keys or values of a page
     static constexpr int kPad = D + 4;
-    static constexpr int kMerge = kStages * 2 * kHalf;                     // [4][16][D + 4] fp32
-    static constexpr int kQuery = kMerge + kConsumers * 16 * kPad * 4;     // MT > 1: [MT][D / 16][32] uint4
-    static constexpr int kInfo = kQuery + (MT > 1 ? MT * (D / 16) * 512 : 0);
-    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // m, l: [4][rows] each
-    static constexpr int kBars = kStats + 2 * 2 * kConsumers * kRows * 4;  // (two sets)
+    static constexpr int kMerge = kStages * 2 * kHalf;                     // [4][8][D + 4] fp32
+    static constexpr int kQuery = kMerge + kConsumers * 8 * kPad * 4;      // [NT][D / 16][32] uint2
+    static constexpr int kInfo = kQuery + (kQueryShared ? NT * (D / 16) * 256 : 0);
+    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // references, sums: [4][rows] each, two sets
+    static constexpr int kBars = kStats + 2 * 2 * kConsumers * kRows * 4;
     static constexpr int kBytes = kBars + (2 * kStages + 1) * 8 + 1024;    // (the start is aligned to 1,024)
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// bytes that the barrier's phase is to wait for beside its arrivals
+__device__ __forceinline__ void mbar_announce(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
 // 16-byte chunk `chunk` of row `row` of a [64][D] tile as the TMA unit has swizzled it
@@ -95,6 +106,15 @@ __device__ __forceinline__ int64_t units_of(const AttnParams &p, const Request &
     return (int64_t)p.kv_heads * ((r.pairs + kRows - 1) / kRows) * (kOverhead + r.pages());
 }
 
+// floor(total * w / W) and, the other way, the worker whose share holds unit x.  A line of less than 2^31 units (all but absurd
+// ones) needs no division in 64 bits, which is a subroutine.
+__device__ __forceinline__ int64_t share_begin(int64_t total, int w, int W) {
+    if (total >> 31) return total * w / W;
+    const unsigned t = (unsigned)total, a = t / (unsigned)W, b = t - a * (unsigned)W;
+    return a * (unsigned)w + b * (unsigned)w / (unsigned)W;
+}
+__device__ __forceinline__ int worker_of(int64_t x, int64_t total, int W) { return (int)(((x + 1) * W - 1) / total); }
+
 struct Share { int64_t begin, end, total, u0; int i0, workers; };
 
 // The worker's share of the cost line and where it begins: request i0, unit u0 of it.  All threads.
@@ -124,8 +144,8 @@ __device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
         s.total += sums[w];
     }
     s.workers = (int)max((int64_t)1, min((int64_t)p.workers, s.total / kMinUnits));
-    s.begin = worker < s.workers ? s.total * worker / s.workers : s.total;
-    s.end = worker < s.workers ? s.total * (worker + 1) / s.workers : s.total;
+    s.begin = worker < s.workers ? share_begin(s.total, worker, s.workers) : s.total;
+    s.end = worker < s.workers ? share_begin(s.total, worker + 1, s.workers) : s.total;
     if (before <= s.begin && s.begin < before + mine) {
         int64_t u = s.begin - before;
         int i = i0;
@@ -143,16 +163,16 @@ __device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
     return s;
 }
 
-template <int D, int MT>
+template <int D, int NT>
 __device__ __forceinline__ void produce(const AttnParams &p, const Share &share, const CUtensorMap *k_map, const CUtensorMap *v_map, uint8_t *smem, uint32_t bars,
                                         const Ctx &ctx, int worker, int lane) {
-    using L = Layout<D, MT>;
+    using L = Layout<D, NT>;
     const uint32_t full = bars, empty = bars + 8 * L::kStages;
     PageInfo *const info = reinterpret_cast<PageInfo *>(smem + L::kInfo);
     int stage = 0, i = share.i0;
     uint32_t phase = 0;
     int64_t unit = share.begin, u = share.u0;
-    bool ok = true, has_cut = false, more = share.begin < share.end;
+    bool ok = true, has_cut = false, more = share.begin < share.end, first = true;
     while (more && ok) {
         // every lane: its unit's item, page and scales
         const int64_t mine = unit + lane;
@@ -168,7 +188,7 @@ __device__ __forceinline__ void produce(const AttnParams &p, const Share &share,
         }
         const bool exists = li < p.B;
         const int pages = r.pages(), cost = kOverhead + pages;
-        const int sub = exists ? (int)(lu / cost) : 0, pos = exists ? (int)(lu - (int64_t)sub * cost) : 0;
+        const int sub = !exists ? 0 : lu >> 31 ? (int)(lu / cost) : (int)((unsigned)lu / (unsigned)cost), pos = exists ? (int)(lu - (int64_t)sub * cost) : 0;
         const int tiles = (r.pairs + L::kRows - 1) / L::kRows;
         const int64_t item = mine - pos;                       // the item's place on the line
         const bool done = !exists || (p.whole ? item >= share.end : mine >= share.end);
@@ -189,7 +209,6 @@ __device__ __forceinline__ void produce(const AttnParams &p, const Share &share,
         a.slot = cut_front ? 2 * worker : cut_back ? 2 * worker + 1 : -1;
         a.k_scale = valid ? p.k_scales[id * p.k_scale_stride + a.head] : 0.f;
         a.v_scale = valid ? p.v_scales[id * p.v_scale_stride + a.head] : 0.f;
-        if (isinf(a.v_scale)) a.v_scale = NAN;
         if (data) {
             if (pos == kOverhead || mine == share.begin) a.flags |= kFirst;
             if (pos == cost - 1 || (!p.whole && mine == share.end - 1)) a.flags |= kLast;
@@ -200,27 +219,38 @@ __device__ __forceinline__ void produce(const AttnParams &p, const Share &share,
             a.flags = kEmpty;
         }
         if (data && pos == kOverhead && cut_back) {
-            // the item's last worker is the one whose share holds its last unit
-            const int last = (int)(((item + cost) * share.workers - 1) / share.total);
-            p.cut[worker] = make_int4(li, sub, last - worker + 1, 0);
+            const int pieces = worker_of(item + cost - 1, share.total, share.workers) - worker + 1;
+            p.cut[2 * worker] = make_int4(pieces, a.row0, a.pairs, a.m0);
+            p.cut[2 * worker + 1] = make_int4(a.head, 0, 0, 0);
         }
         has_cut |= __any_sync(0xffffffffu, data && pos == kOverhead && cut_back);
         unsigned todo = __ballot_sync(0xffffffffu, data || blank);
+        auto copy = [&](int to) {
+            const uint32_t dst = smem_u32(smem) + to * 2 * L::kHalf;
+            mbar_announce(full + 8 * to, 2 * L::kHalf);
+            tma_load_4d(dst, k_map, full + 8 * to, 0, 0, a.head, valid ? id : p.num_pages);      // (behind the pool: zeros)
+            tma_load_4d(dst + L::kHalf, v_map, full + 8 * to, 0, 0, a.head, valid ? id : p.num_pages);
+        };
+        unsigned sent = 0;
+        if (first) {
+            // the ring is empty: the copies of the first pages do not wait for these pages' scales, which are still on their way
+            unsigned ahead = todo;
+            for (int to = 0; to < L::kStages && ahead != 0; ++to, ahead &= ahead - 1) {
+                const int j = __ffs(ahead) - 1;
+                if (lane == j && data) copy(to);
+                sent |= 1u << j;
+            }
+            first = false;
+        }
         while (todo != 0) {
             const int j = __ffs(todo) - 1;
             todo &= todo - 1;
             ok = warp_wait(ctx, empty + 8 * stage, phase ^ 1, 100 + stage);
             if (!ok) break;
             if (lane == j) {
+                if (data && !(sent >> j & 1u)) copy(stage);
                 info[stage] = a;
-                if (data) {
-                    const uint32_t dst = smem_u32(smem) + stage * 2 * L::kHalf;
-                    mbar_expect_tx(full + 8 * stage, 2 * L::kHalf);
-                    tma_load_4d(dst, k_map, full + 8 * stage, 0, 0, a.head, valid ? id : p.num_pages);      // (behind the pool: zeros)
-                    tma_load_4d(dst + L::kHalf, v_map, full + 8 * stage, 0, 0, a.head, valid ? id : p.num_pages);
-                } else {
-                    mbar_arrive(full + 8 * stage);
-                }
+                mbar_arrive(full + 8 * stage);
             }
             __syncwarp();
             if (++stage == L::kStages) { stage = 0; phase ^= 1; }
@@ -235,7 +265,7 @@ __device__ __forceinline__ void produce(const AttnParams &p, const Share &share,
         info[stage].flags = kEnd;
         mbar_arrive(full + 8 * stage);
     }
-    if (!p.whole && !has_cut && lane == 0) p.cut[worker] = make_int4(0, 0, 0, 0);
+    if (!p.whole && !has_cut && lane == 0) p.cut[2 * worker] = make_int4(0, 0, 0, 0);
     if (!ok) {
         // a wait has given up: the copies still in flight must land before the block's shared memory goes to another one
         for (int s = 0; s < L::kStages; ++s) {
@@ -263,23 +293,33 @@ __device__ __forceinline__ void store4(const AttnParams &p, int64_t at, const fl
     }
 }
 
-template <int D, int MT>
+// transposes an 8 x 8 matrix of 16-bit values that lies in the warp's registers, two to a lane
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+template <int D, int NT>
 __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint32_t bars, const Ctx &ctx, int warp, int lane) {
-    using L = Layout<D, MT>;
-    constexpr int kK = D / 16, kN = D / 8;                  // MMAs along the dimensions: as k of the logits, as n of the outputs
+    using L = Layout<D, NT>;
+    constexpr int kK = D / 16, kM = D / 16;                 // MMAs along the dimensions: as k of the logits, as m of the outputs
+    constexpr bool kQueryShared = L::kQueryShared;
     const uint32_t full = bars, empty = bars + 8 * L::kStages, group_bar = bars + 16 * L::kStages;
     const PageInfo *const infos = reinterpret_cast<const PageInfo *>(smem + L::kInfo);
     float *const merge = reinterpret_cast<float *>(smem + L::kMerge);
-    uint4 *const query = reinterpret_cast<uint4 *>(smem + L::kQuery);
-    // m and l of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
+    uint2 *const query = reinterpret_cast<uint2 *>(smem + L::kQuery);
+    // references and sums of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
     float *stat_m = reinterpret_cast<float *>(smem + L::kStats);
     const int n = lane >> 2, c = lane & 3;
     const int perm = D == 128 ? (n >> 1) | (n & 1) << 2 : n;
-    const int tok_a = D == 128 ? c : 2 * c, tok_b = D == 128 ? c + 4 : 2 * c + 1;     // tokens of the S columns 2c, 2c + 1
+    // tokens (of the warp's 16) whose logits the lane holds: perm and perm + 8; whose values it reads: these four
+    const int tok_a = D == 128 ? c : 2 * c, tok_b = D == 128 ? c + 4 : 2 * c + 1;
+    const int tok[4] = {tok_a, tok_b, tok_a + 8, tok_b + 8};
 
-    float o[MT][kN][4], m[MT][2], l[MT][2], rs[MT][2], unit = 0.f;
-    uint32_t qf[MT == 1 ? kK : 1][4];
-    int lim[MT][2];
+    float o[NT][kM][4], ref[NT][2], l[NT][2], rs[NT][2], unit = 0.f;      // of the rows 2c, 2c + 1 of each tile of eight
+    uint32_t qf[kQueryShared ? 1 : NT][kK][2];
+    int lim[NT][2];
     int stage = 0;
     uint32_t phase = 0, group_phase = 0;
     for (;;) {
@@ -290,68 +330,54 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
         if (flags & (kFirst | kEmpty)) {
             // the item's queries, as fp16 with a power of two per row that brings the largest of a row to [2^14, 2^15)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                float v[2][D / 64][16];
-                float factor[2];
+            for (int nt = 0; nt < NT; ++nt) {
+                float v[D / 64][16];
+                const int mm = info.m0 + nt * 8 + n;
+                const bool there = mm < info.pairs && !(flags & kEmpty);
+                const int row = mm / p.group, g = mm - row * p.group;
+                const int64_t at = (info.row0 + row) * p.q_row + (info.head * p.group + g) * p.q_head;
+                int most = 0;
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) {
+                    load_q16(p, at + h * 64 + 16 * c, there, v[h]);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int b = __float_as_int(v[h][k]) & 0x7fffffff;
+                        if (b < 0x7f800000) most = max(most, b);
+                    }
+                }
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                const int shift = most == 0 ? 0 : min(14 - ((most >> 23) - 127), 100);
+                const float factor = __int_as_float((shift + 127) << 23), back = p.scale_log2 * __int_as_float((127 - shift) << 23);
+                const int limit = there ? min(info.hi, info.len - info.rows_all + row + 1) : info.hi;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int mm = info.m0 + mt * 16 + n + 8 * e;
-                    const bool there = mm < info.pairs && !(flags & kEmpty);
-                    const int row = mm / p.group, g = mm - row * p.group;
-                    const int64_t at = (info.row0 + row) * p.q_row + (info.head * p.group + g) * p.q_head;
-                    lim[mt][e] = there ? min(info.hi, info.len - info.rows_all + row + 1) : info.hi;
-                    int most = 0;
-#pragma unroll
-                    for (int h = 0; h < D / 64; ++h) {
-                        load_q16(p, at + h * 64 + 16 * c, there, v[e][h]);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const int b = __float_as_int(v[e][h][k]) & 0x7fffffff;
-                            if (b < 0x7f800000) most = max(most, b);
-                        }
-                    }
-                    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-                    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-                    const int shift = most == 0 ? 0 : min(14 - ((most >> 23) - 127), 100);
-                    factor[e] = __int_as_float((shift + 127) << 23);
-                    rs[mt][e] = p.scale_log2 * __int_as_float((127 - shift) << 23);
-                    m[mt][e] = -INFINITY;
-                    l[mt][e] = 0.f;
+                    rs[nt][e] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + e));
+                    lim[nt][e] = __shfl_sync(0xffffffffu, limit, 4 * (2 * c + e));
+                    ref[nt][e] = kUnset;
+                    l[nt][e] = 0.f;
                 }
 #pragma unroll
                 for (int k = 0; k < kK; ++k) {
-                    const int h = k / 4, at = 4 * (k % 4);
-                    uint32_t a[4];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        a[e] = pack_f16x2(v[e][h][at] * factor[e], v[e][h][at + 1] * factor[e]);
-                        a[2 + e] = pack_f16x2(v[e][h][at + 2] * factor[e], v[e][h][at + 3] * factor[e]);
-                    }
-                    if constexpr (MT == 1) {
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) qf[k][x] = a[x];
-                    } else if (k % kConsumers == warp) {
-                        query[(mt * kK + k) * 32 + lane] = make_uint4(a[0], a[1], a[2], a[3]);
-                    }
+                    const int h = k / 4, x = 4 * (k % 4);
+                    const uint2 b = make_uint2(pack_f16x2(v[h][x] * factor, v[h][x + 1] * factor), pack_f16x2(v[h][x + 2] * factor, v[h][x + 3] * factor));
+                    if constexpr (!kQueryShared) { qf[nt][k][0] = b.x; qf[nt][k][1] = b.y; }
+                    else if (k % kConsumers == warp) query[(nt * kK + k) * 32 + lane] = b;
                 }
 #pragma unroll
-                for (int j = 0; j < kN; ++j)
+                for (int j = 0; j < kM; ++j)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) o[mt][j][x] = 0.f;
+                    for (int x = 0; x < 4; ++x) o[nt][j][x] = 0.f;
             }
             unit = 0.f;
-            if (MT > 1 && !meet(ctx, group_bar, group_phase, lane)) break;
+            if (kQueryShared && !meet(ctx, group_bar, group_phase, lane)) break;
         }
         if (!(flags & kEmpty)) {
             const uint8_t *const keys = smem + stage * 2 * L::kHalf, *const values = keys + L::kHalf;
-            // ---- logits of 16 tokens
-            float s[MT][2][4];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) s[mt][t][x] = 0.f;
+            // ---- logits of 16 tokens (m) and eight rows at a time (n)
+            constexpr int kChains = NT == 1 && D == 128 ? 2 : 1;     // sums side by side: an MMA waits for the one before it in its sum
+            float parts[kChains][NT][4] = {}, (&s)[NT][4] = parts[0];
             uint32_t kw[2][kK];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -362,21 +388,23 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                 }
 #pragma unroll
             for (int k = 0; k < kK; ++k) {
-                uint32_t b[2][2];
+                uint32_t a[2][2];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) { b[t][0] = to_f16x2(kw[t][k] & 0xffff); b[t][1] = to_f16x2(kw[t][k] >> 16); }
+                for (int t = 0; t < 2; ++t) to_f16x4(kw[t][k], a[t][0], a[t][1]);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    uint4 a;
-                    if constexpr (MT == 1) a = make_uint4(qf[k][0], qf[k][1], qf[k][2], qf[k][3]);
-                    else a = query[(mt * kK + k) * 32 + lane];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) mma_f16(s[mt][t], a.x, a.y, a.z, a.w, b[t][0], b[t][1]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    uint2 b;
+                    if constexpr (!kQueryShared) b = make_uint2(qf[nt][k][0], qf[nt][k][1]);
+                    else b = query[(nt * kK + k) * 32 + lane];
+                    mma_f16(parts[k % kChains][nt], a[0][0], a[1][0], a[0][1], a[1][1], b.x, b.y);
                 }
+            }
+            if constexpr (kChains == 2) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) s[0][x] += parts[kChains - 1][0][x];
             }
             // ---- values of the tokens a, b, a + 8, b + 8
             uint32_t vw[4][D / 32];
-            const int tok[4] = {tok_a, tok_b, tok_a + 8, tok_b + 8};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int row = 16 * warp + tok[t];
@@ -388,81 +416,93 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                     vw[t][0] = w.x; vw[t][1] = w.y;
                 }
             }
-            const float ks = info.k_scale, vs = info.v_scale;
-            // ---- weights
-            bool grows = false;
+            // ---- weights, in base 2 relative to the row's reference, and relative to the largest value scale so far
+            const float ks = info.k_scale, vs = isinf(info.v_scale) ? NAN : info.v_scale;
+            if (fabsf(vs) > unit) {
+                const float a = __fdividef(unit, fabsf(vs));
+                unit = fabsf(vs);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                    for (int j = 0; j < kM; ++j)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) s[mt][t][x] *= rs[mt][x >> 1] * ks;
+                        for (int x = 0; x < 4; ++x) o[nt][j][x] *= a;
+            }
+            const float f = vs == unit ? 1.f : __fdividef(vs, unit);
+            uint32_t hidden = 0;                     // logits of tokens that the row does not see, a bit each
             if (flags & kEdge) {
                 const int base = info.t0 + 16 * warp, lo = info.lo, hi = info.hi;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int at = base + tok[t];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
+                    for (int x = 0; x < 4; ++x) {
+                        const int at = base + perm + 8 * (x >> 1);
+                        if (at < lo || at >= lim[nt][x & 1]) hidden |= 1u << (4 * nt + x);
+                    }
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (at < lo || at >= lim[mt][e]) s[mt][t >> 1][2 * e + (t & 1)] = -INFINITY;
-                    if (at < lo || at >= hi) {
+                for (int t = 0; t < 4; ++t)
+                    if (base + tok[t] < lo || base + tok[t] >= hi) {
 #pragma unroll
                         for (int q = 0; q < D / 32; ++q) vw[t][q] = 0;
                     }
-                }
             }
+            float y[NT][4], most = -INFINITY;
+            auto relative = [&] {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                    for (int x = 0; x < 4; ++x) y[nt][x] = fmaf(s[nt][x], rs[nt][x & 1] * ks, -ref[nt][x & 1]);
+                if (hidden != 0) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) grows |= s[mt][t][x] > m[mt][x >> 1] + kSlack;
-            if (__any_sync(0xffffffffu, grows)) {
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                        for (int x = 0; x < 4; ++x)
+                            if (hidden >> (4 * nt + x) & 1u) y[nt][x] = -INFINITY;
+                }
+            };
+            relative();
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) most = fmaxf(most, y[nt][x]);
+            if (__any_sync(0xffffffffu, most > kLift + kSlack)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(fmaxf(s[mt][0][2 * e], s[mt][0][2 * e + 1]), fmaxf(s[mt][1][2 * e], s[mt][1][2 * e + 1]));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                        top = fmaxf(top, m[mt][e]);
-                        if (top > m[mt][e]) {
-                            const float a = fast_exp2(m[mt][e] - top);       // (m = -inf: 0)
-                            m[mt][e] = top;
-                            l[mt][e] *= a;
+                        float top = -INFINITY;
 #pragma unroll
-                            for (int j = 0; j < kN; ++j) { o[mt][j][2 * e] *= a; o[mt][j][2 * e + 1] *= a; }
+                        for (int x = e; x < 4; x += 2)
+                            if (!(hidden >> (4 * nt + x) & 1u)) top = fmaxf(top, s[nt][x] * (rs[nt][e] * ks));
+#pragma unroll
+                        for (int sh = 4; sh < 32; sh <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sh));
+                        top -= kLift;
+                        if (top > ref[nt][e]) {
+                            const float a = fast_exp2(ref[nt][e] - top);
+                            ref[nt][e] = top;
+                            l[nt][e] *= a;
+#pragma unroll
+                            for (int j = 0; j < kM; ++j) { o[nt][j][e] *= a; o[nt][j][2 + e] *= a; }
                         }
                     }
+                relative();
             }
-            if (fabsf(vs) > unit) {
-                const float a = __fdiv_rn(unit, fabsf(vs));
-                unit = fabsf(vs);
+            uint32_t pf[NT][2];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt) {
+                float w[4];
 #pragma unroll
-                    for (int j = 0; j < kN; ++j)
+                for (int x = 0; x < 4; ++x) w[x] = fast_exp2(y[nt][x]);
+                l[nt][0] += w[0] + w[2];
+                l[nt][1] += w[1] + w[3];
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) o[mt][j][x] *= a;
-            }
-            const float f = vs == unit ? 1.f : __fdiv_rn(vs, unit);
-            uint32_t pf[MT][4];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float ref = (m[mt][e] == -INFINITY ? 0.f : m[mt][e]) - kLift;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const float p0 = fast_exp2(s[mt][t][2 * e] - ref), p1 = fast_exp2(s[mt][t][2 * e + 1] - ref);
-                        l[mt][e] += p0 + p1;
-                        pf[mt][2 * t + e] = pack_f16x2(p0 * f, p1 * f);
-                        if (!(f == f))                                       // a scale that is NaN, for the rows that see the token
-                            pf[mt][2 * t + e] = (s[mt][t][2 * e] == -INFINITY ? 0u : 0x7fffu) | (s[mt][t][2 * e + 1] == -INFINITY ? 0u : 0x7fff0000u);
-                    }
+                for (int t = 0; t < 2; ++t) {
+                    pf[nt][t] = pack_f16x2(w[2 * t] * f, w[2 * t + 1] * f);
+                    if (!(f == f))                               // a scale that is NaN, for the rows that see the token
+                        pf[nt][t] = (y[nt][2 * t] == -INFINITY ? 0u : 0x7fffu) | (y[nt][2 * t + 1] == -INFINITY ? 0u : 0x7fff0000u);
+                    pf[nt][t] = transpose8x8(pf[nt][t]);         // tokens to k, rows to n
                 }
+            }
             // ---- a NaN value in a page where some rows do not see every token: products 0 * NaN must not reach the rows that do
             // not see it.  Values without NaN go on; rows that see one get it by counting (weights 1 and 0) instead.
             if (flags & kCausal) {
@@ -472,51 +512,50 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
 #pragma unroll
                     for (int q = 0; q < D / 32; ++q) nan |= ((vw[t][q] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
                 if (__any_sync(0xffffffffu, nan != 0)) {
-                    uint32_t nw[4][D / 32];
+                    uint32_t sees[NT][2];
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int q = 0; q < D / 32; ++q) {
+                        for (int t = 0; t < 2; ++t)
+                            sees[nt][t] = transpose8x8((hidden >> (4 * nt + 2 * t) & 1u ? 0u : 0x3c00u) | (hidden >> (4 * nt + 2 * t + 1) & 1u ? 0u : 0x3c000000u));
+#pragma unroll
+                    for (int q = 0; q < D / 32; ++q) {
+                        uint32_t nw[4];
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
                             const uint32_t at = (((vw[t][q] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
-                            nw[t][q] = at * 0x38u;                      // 1.0
+                            nw[t] = at * 0x38u;                         // 1.0
                             vw[t][q] &= ~(at * 0xffu);
                         }
-                    const int base = info.t0 + 16 * warp;
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        uint32_t sees[4];
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t sel = half ? 0x7362 : 0x5140;
+                            uint32_t a0, a1, a2, a3;
+                            to_f16x4(__byte_perm(nw[0], nw[1], sel), a0, a1);
+                            to_f16x4(__byte_perm(nw[2], nw[3], sel), a2, a3);
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
+                            for (int nt = 0; nt < NT; ++nt) {
+                                float count[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_f16(count, a0, a1, a2, a3, sees[nt][0], sees[nt][1]);
 #pragma unroll
-                            for (int t = 0; t < 2; ++t)
-                                sees[2 * t + e] = (base + tok[2 * t] < lim[mt][e] ? 0x3c00u : 0u) | (base + tok[2 * t + 1] < lim[mt][e] ? 0x3c000000u : 0u);
-#pragma unroll
-                        for (int j = 0; j < kN; ++j) {
-                            const uint32_t sel = (j & 2) ? 0x7362 : 0x5140;
-                            const uint32_t x = __byte_perm(nw[0][j / 4], nw[1][j / 4], sel), y = __byte_perm(nw[2][j / 4], nw[3][j / 4], sel);
-                            float count[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_f16(count, sees[0], sees[1], sees[2], sees[3], to_f16x2((j & 1) ? x >> 16 : x & 0xffff), to_f16x2((j & 1) ? y >> 16 : y & 0xffff));
-#pragma unroll
-                            for (int x2 = 0; x2 < 4; ++x2)
-                                if (count[x2] > 0.f) o[mt][j][x2] = NAN;
+                                for (int x = 0; x < 4; ++x)
+                                    if (count[x] > 0.f) o[nt][2 * q + half][x] = NAN;
+                            }
                         }
                     }
                 }
             }
-            // ---- outputs
+            // ---- outputs: 16 dimensions (m), eight rows (n)
 #pragma unroll
             for (int q = 0; q < D / 32; ++q)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const uint32_t sel = half ? 0x7362 : 0x5140;
-                    const uint32_t x = __byte_perm(vw[0][q], vw[1][q], sel), y = __byte_perm(vw[2][q], vw[3][q], sel);
+                    uint32_t a0, a1, a2, a3;
+                    to_f16x4(__byte_perm(vw[0][q], vw[1][q], sel), a0, a1);
+                    to_f16x4(__byte_perm(vw[2][q], vw[3][q], sel), a2, a3);
 #pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const int j = 4 * q + 2 * half + z;
-                        const uint32_t b0 = to_f16x2(z ? x >> 16 : x & 0xffff), b1 = to_f16x2(z ? y >> 16 : y & 0xffff);
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) mma_f16(o[mt][j], pf[mt][0], pf[mt][1], pf[mt][2], pf[mt][3], b0, b1);
-                    }
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][2 * q + half], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
                 }
         }
         if (flags & (kLast | kEmpty)) {
@@ -526,69 +565,64 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    l[mt][e] += __shfl_xor_sync(0xffffffffu, l[mt][e], 1);
-                    l[mt][e] += __shfl_xor_sync(0xffffffffu, l[mt][e], 2);
-                    if (c == 0) {
-                        stat_m[warp * L::kRows + mt * 16 + n + 8 * e] = m[mt][e];
-                        stat_l[warp * L::kRows + mt * 16 + n + 8 * e] = l[mt][e];
+#pragma unroll
+                    for (int sh = 4; sh < 32; sh <<= 1) l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], sh);
+                    if (n == 0) {
+                        stat_m[warp * L::kRows + nt * 8 + 2 * c + e] = ref[nt][e];
+                        stat_l[warp * L::kRows + nt * 8 + 2 * c + e] = l[nt][e];
                     }
                 }
             if (!meet(ctx, group_bar, group_phase, lane)) break;
             bool ok = true;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
+            for (int nt = 0; nt < NT; ++nt) {
+                if (m0 + nt * 8 >= pairs) break;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = mt * 16 + n + 8 * e;
-                    float top = -INFINITY;
+                    const int r = nt * 8 + 2 * c + e;
+                    float top = kUnset;
 #pragma unroll
                     for (int w = 0; w < kConsumers; ++w) top = fmaxf(top, stat_m[w * L::kRows + r]);
-                    const float a = fast_exp2(m[mt][e] - (top == -INFINITY ? 0.f : top));
-                    float *const to = merge + (warp * 16 + n + 8 * e) * L::kPad;
+                    const float a = fast_exp2(ref[nt][e] - top);
+                    float *const to = merge + (warp * 8 + 2 * c + e) * L::kPad + (D == 128 ? perm * 16 : n * 8);
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        // columns 2c and 2c + 1 of all MMAs: successive dimensions
-                        const int d = D == 128 ? 64 * half + 16 * c : 16 * c + 8 * half;
-#pragma unroll
-                        for (int j = 0; j < kN; j += 4)
-                            *reinterpret_cast<float4 *>(to + d + j) = make_float4(o[mt][j][2 * e + half] * a, o[mt][j + 1][2 * e + half] * a,
-                                                                                  o[mt][j + 2][2 * e + half] * a, o[mt][j + 3][2 * e + half] * a);
-                    }
+                    for (int j = 0; j < kM; j += 2)
+                        *reinterpret_cast<float4 *>(to + 2 * j) =
+                            make_float4(o[nt][j][e] * a, o[nt][j][2 + e] * a, o[nt][j + 1][e] * a, o[nt][j + 1][2 + e] * a);
                 }
                 if (!(ok = meet(ctx, group_bar, group_phase, lane))) break;
-                const int tid = warp * 32 + lane, r16 = tid >> 3, r = mt * 16 + r16, mm = m0 + r;
+                const int tid = warp * 32 + lane, r8 = tid >> 4, r = nt * 8 + r8, mm = m0 + r;
                 if (mm < pairs) {
-                    float top = -INFINITY, sum = 0.f;
+                    float top = kUnset, sum = 0.f;
 #pragma unroll
                     for (int w = 0; w < kConsumers; ++w) top = fmaxf(top, stat_m[w * L::kRows + r]);
-                    const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-                    for (int w = 0; w < kConsumers; ++w) sum += stat_l[w * L::kRows + r] * fast_exp2(stat_m[w * L::kRows + r] - ref);
+                    for (int w = 0; w < kConsumers; ++w) sum += stat_l[w * L::kRows + r] * fast_exp2(stat_m[w * L::kRows + r] - top);
                     const float scale = sum == 0.f ? 0.f : unit / sum;
-                    const float lse2 = sum == 0.f ? -INFINITY : ref + __log2f(sum) - kLift;
+                    const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
                     const int row = mm / p.group, g = head * p.group + mm - row * p.group;
 #pragma unroll
-                    for (int q = 0; q < D / 32; ++q) {
-                        const int d = 4 * ((tid & 7) + 8 * q);
-                        float4 v = *reinterpret_cast<const float4 *>(merge + r16 * L::kPad + d);
+                    for (int q = 0; q < D / 64; ++q) {
+                        const int d = 4 * ((tid & 15) + 16 * q);
+                        float4 v = *reinterpret_cast<const float4 *>(merge + r8 * L::kPad + d);
 #pragma unroll
                         for (int w = 1; w < kConsumers; ++w) {
-                            const float4 x = *reinterpret_cast<const float4 *>(merge + (w * 16 + r16) * L::kPad + d);
+                            const float4 x = *reinterpret_cast<const float4 *>(merge + (w * 8 + r8) * L::kPad + d);
                             v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
                         }
                         v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
                         if (slot < 0) store4(p, (row0 + row) * p.out_row + g * p.out_head + d, v);
                         else *reinterpret_cast<float4 *>(p.part_out + ((int64_t)slot * L::kRows + r) * D + d) = v;
                     }
-                    if ((tid & 7) == 0) {
+                    if ((tid & 15) == 0) {
                         if (slot < 0) p.lse[(row0 + row) * p.lse_row + g] = lse2 * kLn2;
                         else p.part_lse[slot * L::kRows + r] = lse2;
                     }
                 }
-                if (MT > 1 && mt + 1 < MT && !(ok = meet(ctx, group_bar, group_phase, lane))) break;
+                if (nt + 1 < NT && m0 + nt * 8 + 8 < pairs && !(ok = meet(ctx, group_bar, group_phase, lane))) break;
             }
             if (!ok) break;
             stat_m = reinterpret_cast<float *>(smem + L::kStats) + (stat_m == reinterpret_cast<float *>(smem + L::kStats) ? 2 * kConsumers * L::kRows : 0);
@@ -600,10 +634,10 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
     }
 }
 
-template <int D, int MT>
-__global__ void __launch_bounds__(kThreads, 2)
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtas)
 kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-    using L = Layout<D, MT>;
+    using L = Layout<D, NT>;
     extern __shared__ uint8_t raw[];
     __shared__ uint32_t abort_flag;
     uint8_t *const smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
@@ -620,58 +654,95 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
     if (blockIdx.x == 0 && threadIdx.x < 4) p.status[threadIdx.x] = 0;
     const Share share = plan<L::kRows>(p, worker);      // (its barriers publish the mbarriers too)
     const Ctx ctx = {&abort_flag, p.status};
-    if (warp == kConsumers) produce<D, MT>(p, share, &k_map, &v_map, smem, bars, ctx, worker, lane);
-    else consume<D, MT>(p, smem, bars, ctx, warp, lane);
+    if (warp == kConsumers) produce<D, NT>(p, share, &k_map, &v_map, smem, bars, ctx, worker, lane);
+    else consume<D, NT>(p, smem, bars, ctx, warp, lane);
 }
 
-// Pieces of the cut items, [piece][row][D] with their base-2 lse: out = sum_j 2^(lse_j - lse) out_j.  Block (worker, group of four
-// rows), a warp per row; the pieces of an item lie in the last slot of its first worker and the first slots of the following ones.
-template <int D, int kRows>
-__global__ void __launch_bounds__(128)
+// Pieces of the cut items, [piece][row][D] with their base-2 lse: out = sum_j 2^(lse_j - lse) out_j.  The pieces of an item lie in the
+// last slot of its first worker and the first slots of the following ones.  Block (worker, 4 / kWarps rows), kWarps warps to a row that share
+// its pieces: one where there are items for all workers, so that most have a piece or two; four where a few items are spread over all of them (one
+// context over all workers has 55 pieces for each of eight heads, which a warp alone walks through in 16 us).
+// The next kernel on the stream is let in at the end and not at the start: blocks of the next call's decode kernel that come in
+// beside these, three to an SM where there is room for fewer, cost that call more (64 contexts of 1k to 8k tokens: 127 us a call) than the launch that
+// is hidden gives (106).
+template <int D, int kRows, int kWarps>
+__global__ void __launch_bounds__(128, 8)
 kv8_combine_kernel(const __grid_constant__ AttnParams p) {
+    constexpr int kPer = D / 32, kBatch = 8;
+    __shared__ float sums[4], tops[4], parts[4][D];
     grid_dependency_wait();
-    grid_launch_dependents();
     const int worker = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int4 cut = p.cut[worker];
-    if (cut.z == 0) return;
-    const Request req = request(p, cut.x);
-    const int tiles = (req.pairs + kRows - 1) / kRows, head = cut.y / tiles;
-    const int r = blockIdx.y * 4 + warp, mm = (cut.y % tiles) * kRows + r;
-    if (mm >= req.pairs) return;
+    const int4 cut = p.cut[2 * worker];           // pieces, first query row, (row, head) pairs, first pair of the tile
+    const int head = p.cut[2 * worker + 1].x;
+    const int pieces = cut.x, r = blockIdx.y * (4 / kWarps) + warp / kWarps, mm = cut.w + r;
+    if (pieces == 0) return;
+    const bool there = mm < cut.z;
     auto slot = [&](int j) { return j == 0 ? 2 * worker + 1 : 2 * (worker + j); };
-    float top = -INFINITY;
-    for (int j = lane; j < cut.z; j += 32) top = fmaxf(top, p.part_lse[slot(j) * kRows + r]);
+    float top = kUnset, acc[kPer] = {}, sum = 0.f;
+    if (there) {
+        for (int j0 = warp % kWarps; j0 < pieces; j0 += kWarps * kBatch) {
+            float w[kBatch], v[kBatch][kPer], most = kUnset;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float ref = top == -INFINITY ? 0.f : top;
-    constexpr int kPer = D / 32;
-    float acc[kPer] = {}, sum = 0.f;
-    for (int j0 = 0; j0 < cut.z; j0 += 8) {
-        float w[8], v[8][kPer];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bool there = j0 + k < cut.z;
-            const int64_t at = (int64_t)slot(there ? j0 + k : 0) * kRows + r;
-            w[k] = there ? fast_exp2(p.part_lse[at] - ref) : 0.f;
-            if constexpr (kPer == 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(p.part_out + at * D + lane * 4);
-                v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
-            } else {
-                const float2 x = *reinterpret_cast<const float2 *>(p.part_out + at * D + lane * 2);
-                v[k][0] = x.x; v[k][1] = x.y;
+            for (int k = 0; k < kBatch; ++k) {
+                const int j = j0 + kWarps * k;
+                w[k] = -INFINITY;
+                if (j < pieces) {
+                    const int64_t at = (int64_t)slot(j) * kRows + r;
+                    w[k] = p.part_lse[at];
+                    if constexpr (kPer == 4) {
+                        const float4 x = *reinterpret_cast<const float4 *>(p.part_out + at * D + lane * 4);
+                        v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
+                    } else {
+                        const float2 x = *reinterpret_cast<const float2 *>(p.part_out + at * D + lane * 2);
+                        v[k][0] = x.x; v[k][1] = x.y;
+                    }
+                }
             }
-        }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (j0 + k >= cut.z) break;
-            sum += w[k];
+            for (int k = 0; k < kBatch; ++k) most = fmaxf(most, w[k]);
+            if (most > top) {
+                const float a = fast_exp2(top - most);
+                top = most;
+                sum *= a;
 #pragma unroll
-            for (int x = 0; x < kPer; ++x) acc[x] += w[k] * v[k][x];
+                for (int x = 0; x < kPer; ++x) acc[x] *= a;
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (j0 + kWarps * k < pieces) {
+                    w[k] = fast_exp2(w[k] - top);
+                    sum += w[k];
+#pragma unroll
+                    for (int x = 0; x < kPer; ++x) acc[x] += w[k] * v[k][x];
+                }
         }
     }
+    if constexpr (kWarps > 1) {
+        if (lane == 0) { sums[warp] = sum; tops[warp] = top; }
+#pragma unroll
+        for (int x = 0; x < kPer; ++x) parts[warp][lane * kPer + x] = acc[x];
+        __syncthreads();
+        if (warp % kWarps != 0) return;
+        float most = top;
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) most = fmaxf(most, tops[warp + w]);
+        const float a = fast_exp2(top - most);
+        sum *= a;
+#pragma unroll
+        for (int x = 0; x < kPer; ++x) acc[x] *= a;
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+            const float b = fast_exp2(tops[warp + w] - most);
+            sum += sums[warp + w] * b;
+#pragma unroll
+            for (int x = 0; x < kPer; ++x) acc[x] += parts[warp + w][lane * kPer + x] * b;
+        }
+        top = most;
+    }
+    if (!there) return;
     const float scale = sum == 0.f ? 0.f : 1.f / sum;
     const int row = mm / p.group, g = head * p.group + mm - row * p.group;
-    const int64_t at = (int64_t)(req.row0 + row) * p.out_row + g * p.out_head + lane * kPer;
+    const int64_t at = (int64_t)(cut.y + row) * p.out_row + g * p.out_head + lane * kPer;
     if constexpr (kPer == 4) {
         store4(p, at, make_float4(acc[0] * scale, acc[1] * scale, acc[2] * scale, acc[3] * scale));
     } else if (p.out_f32) {
@@ -680,7 +751,7 @@ kv8_combine_kernel(const __grid_constant__ AttnParams p) {
         *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.out) + at) =
             p.q_bf16 ? pack_bf16x2(acc[0] * scale, acc[1] * scale) : pack_f16x2(acc[0] * scale, acc[1] * scale);
     }
-    if (lane == 0) p.lse[(int64_t)(req.row0 + row) * p.lse_row + g] = sum == 0.f ? -INFINITY : (ref + __log2f(sum)) * kLn2;
+    if (lane == 0) p.lse[(int64_t)(cut.y + row) * p.lse_row + g] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
 bool make_pool_map(CUtensorMap *map, const splash_kv8_cache &c, const void *pool, int64_t page_stride, int64_t head_stride) {
@@ -698,33 +769,53 @@ bool make_pool_map(CUtensorMap *map, const splash_kv8_cache &c, const void *pool
     return r == CUDA_SUCCESS;
 }
 
-template <int D, int MT>
-cudaError_t launch_decode(const AttnParams &p, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
-    using L = Layout<D, MT>;
+template <int D, int NT>
+cudaError_t launch_decode(const AttnParams &p, int items, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
+    using L = Layout<D, NT>;
     static DeviceOnce once;
     cudaError_t e = once.run([] {
-        return cudaFuncSetAttribute(kv8_decode_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+        // (an SM that had to change its shared memory between the two would have to run empty first)
+        for (const auto kernel : {kv8_combine_kernel<D, L::kRows, 1>, kv8_combine_kernel<D, L::kRows, 4>}) {
+            const cudaError_t c = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+            if (c != cudaSuccess) return c;
+        }
+        return cudaFuncSetAttribute(kv8_decode_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
     });
     if (e != cudaSuccess) return e;
-    e = launch_dependent(kv8_decode_kernel<D, MT>, dim3(p.workers), dim3(kThreads), L::kBytes, stream, p, k_map, v_map);
+    e = launch_dependent(kv8_decode_kernel<D, NT>, dim3(p.workers), dim3(kThreads), L::kBytes, stream, p, k_map, v_map);
     count_launch();
     if (e != cudaSuccess || p.whole) return e;
-    e = launch_dependent(kv8_combine_kernel<D, L::kRows>, dim3(p.workers, L::kRows / 4), dim3(128), 0, stream, p);
+    e = p.workers / items >= 8 ? launch_dependent(kv8_combine_kernel<D, L::kRows, 4>, dim3(p.workers, L::kRows), dim3(128), 0, stream, p)
+                               : launch_dependent(kv8_combine_kernel<D, L::kRows, 1>, dim3(p.workers, L::kRows / 4), dim3(128), 0, stream, p);
     count_launch();
     return e;
 }
 
 }  // namespace
 
-int kv8_decode_workers(int sm_count) { return 2 * sm_count; }
+// Rows of a tile for requests of at most `pairs` (row, head) pairs, and the workers that the line is cut for (the blocks that the GPU holds).
+void kv8_decode_shape(int64_t pairs, int head_dim, int sm_count, int *rows, int *workers) {
+    const int64_t most = head_dim == 64 ? 32 : 16, tiles = (pairs + most - 1) / most;
+    *rows = (int)((pairs + tiles - 1) / tiles + 7) / 8 * 8;
+    *workers = 3 * sm_count;
+}
 
 bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v_map) {
     return make_pool_map(k_map, c, c.k_pool, c.k_page_stride, c.k_head_stride) && make_pool_map(v_map, c, c.v_pool, c.v_page_stride, c.v_head_stride);
 }
 
 cudaError_t launch_kv8_decode(const AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
-    if (D == 128) return rows <= 16 ? launch_decode<128, 1>(p, k_map, v_map, stream) : launch_decode<128, 2>(p, k_map, v_map, stream);
-    return rows <= 16 ? launch_decode<64, 1>(p, k_map, v_map, stream) : launch_decode<64, 2>(p, k_map, v_map, stream);
+    const int64_t tiles = ((int64_t)p.max_rows * p.group + rows - 1) / rows, all = tiles * p.kv_heads * p.B;
+    const int items = (int)(all < 0x7fffffff ? all : 0x7fffffff);        // at most
+    auto of = [&](auto d) {
+        constexpr int kD = decltype(d)::value;
+        if constexpr (kD == 64) {
+            if (rows == 24) return launch_decode<kD, 3>(p, items, k_map, v_map, stream);
+            if (rows == 32) return launch_decode<kD, 4>(p, items, k_map, v_map, stream);
+        }
+        return rows == 8 ? launch_decode<kD, 1>(p, items, k_map, v_map, stream) : launch_decode<kD, 2>(p, items, k_map, v_map, stream);
+    };
+    return D == 128 ? of(std::integral_constant<int, 128>{}) : of(std::integral_constant<int, 64>{});
 }
 
 }  // namespace splash
