@@ -21,6 +21,9 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
     return r;
 }
 
+constexpr float kLift = 7.f, kSlack = 8.f;          // softmax weights are kept below 2^(kLift + kSlack) = 2^15
+constexpr float kUnset = -1e38f;                    // reference of a row that has seen no token: any logit is far above it
+
 // ---- attention -----------------------------------------------------------------------------------------------------------
 
 struct AttnParams {

@@ -15,6 +15,8 @@ cudaError_t launch_kv8_append(const splash_kv8_cache &cache, int32_t dtype, int6
                               int64_t v_row, int64_t v_head, const int64_t *slot_map, int sm_count, cudaStream_t stream);
 void kv8_decode_shape(int64_t pairs, int head_dim, int sm_count, int *rows, int *workers);
 bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v_map);
+int kv8_chunk_rows();
+cudaError_t launch_kv8_chunk(const kv8::AttnParams &p, const splash_kv8_cache &cache, cudaStream_t stream);
 cudaError_t launch_kv8_decode(const kv8::AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream);
 
 namespace {
@@ -94,9 +96,26 @@ View carve(void *base, int workers, int rows, int D) {
     return v;
 }
 
-View carve(void *base, const splash_kv8_cache *c, const splash_kv8_query *s, int sms, int &rows, int &workers) {
-    kv8_decode_shape((int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads), c->head_dim, sms, &rows, &workers);
-    return carve(base, workers, rows, c->head_dim);
+// How a call runs: requests of up to kDecodePairs (row, head) pairs on the decode kernel, the others, if there may be any, on the kernel for chunks.
+// (A page and its 256 rows take the latter what three or four of the former's tiles take: where the two meet is measured at the constant.)
+constexpr int kDecodePairs = 64;
+
+struct Plan { int rows, workers, chunk_workers; int64_t pairs; };
+
+Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
+    Plan p;
+    p.pairs = (int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads);
+    kv8_decode_shape(p.pairs < kDecodePairs ? p.pairs : kDecodePairs, c->head_dim, sms, &p.rows, &p.workers);
+    p.chunk_workers = p.pairs > kDecodePairs ? sms : 0;
+    return p;
+}
+
+// One region serves both kernels: the second writes only when the first's combine kernel is done.
+View carve(void *base, const splash_kv8_cache *c, const Plan &p) {
+    View v = carve(base, p.workers, p.rows, c->head_dim);
+    const size_t chunk = carve(base, p.chunk_workers, kv8_chunk_rows(), c->head_dim).bytes;
+    if (chunk > v.bytes) v.bytes = chunk;
+    return v;
 }
 
 }  // namespace
@@ -164,8 +183,7 @@ size_t splash_kv8_attention_workspace_bytes(const splash_kv8_cache *cache, const
     if (check_cache(cache) != SPLASH_OK || check_query(cache, query) != SPLASH_OK) return 0;
     int sms = 0;
     if (usable_device(sms) != SPLASH_OK) return 0;
-    int rows, workers;
-    return carve(nullptr, cache, query, sms, rows, workers).bytes;
+    return carve(nullptr, cache, plan_call(cache, query, sms)).bytes;
 }
 
 int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *query, const void *q, const int32_t *block_table,
@@ -184,8 +202,8 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
     int sms = 0;
     rc = usable_device(sms);
     if (rc != SPLASH_OK) return rc;
-    int rows, workers;
-    const View v = carve(workspace, cache, query, sms, rows, workers);
+    const Plan plan = plan_call(cache, query, sms);
+    const View v = carve(workspace, cache, plan);
     if (workspace_bytes < v.bytes) {
         set_error("workspace has %zu bytes, %zu needed", workspace_bytes, v.bytes);
         return SPLASH_INVALID_ARG;
@@ -204,11 +222,19 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
     p.num_pages = cache->num_pages; p.max_rows = query->max_q_rows;
     p.q_bf16 = query->dtype == SPLASH_DTYPE_BF16; p.out_f32 = query->out_dtype == SPLASH_DTYPE_FP32;
     p.whole = query->table_width <= kWholeRequestPages;
-    p.workers = workers;
-    p.min_pairs = 1; p.max_pairs = 0x7fffffff;
+    p.workers = plan.workers;
+    p.min_pairs = 1; p.max_pairs = kDecodePairs;
     p.scale_log2 = query->softmax_scale * umma::kLog2e;
     p.status = v.status; p.cut = v.cut; p.part_lse = v.lse; p.part_out = v.out;
-    return launched(launch_kv8_decode(p, cache->head_dim, rows, k_map, v_map, static_cast<cudaStream_t>(stream)));
+    cudaError_t e = launch_kv8_decode(p, cache->head_dim, plan.rows, k_map, v_map, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess && plan.chunk_workers > 0) {
+        const View w = carve(workspace, plan.chunk_workers, kv8_chunk_rows(), cache->head_dim);
+        p.workers = plan.chunk_workers;
+        p.min_pairs = kDecodePairs + 1; p.max_pairs = 0x7fffffff;
+        p.cut = w.cut; p.part_lse = w.lse; p.part_out = w.out;
+        e = launch_kv8_chunk(p, *cache, static_cast<cudaStream_t>(stream));
+    }
+    return launched(e);
 }
 
 }  // extern "C"

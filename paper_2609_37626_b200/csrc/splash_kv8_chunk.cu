@@ -1,0 +1,785 @@
+// Attention of many query rows (chunks of prompts) over a paged cache of keys and values in e4m3 with a scale per (page, head).
+//
+// The (row, head) pairs of a request and key head, m = row * group + head, are cut in tiles of 256; an item of work is (request, key head, tile).
+// Tokens come 128 at a time (two pages).  Tensor cores bound it: per 128 tokens 2 x 16 MMAs of 128 x 128 x 16 take 2,048 cycles, and the
+// 32,768 exponentials as long.  One block an SM, 14 warps:
+//   - 4 converter warps read codes (16 bytes a lane), widen them to fp16 (exact) and lay them out in shared memory, keys K-major and values MN-major in
+//     the 128-byte swizzle, two stages each.  They pay for 256 query rows at once: per code half a conversion and two bytes of stores.
+//   - 1 warp issues tcgen05.mma: S = Q K^T from shared memory into tensor memory; O += P V with P read from tensor memory, where the softmax
+//     leaves it over S.  The halves of the tile (128 rows each) take turns: while one's softmax runs, the tensor cores work for the other.
+//   - 2 x 4 softmax warps, a thread per row: p = 2^(x - m + 7) with a reference m that moves only when a logit exceeds it by 8 (then O, the sum, and what
+//     has been written of P are rescaled), p rounded to fp16, value scales folded into p as v_scale / U with U the largest so far.
+//   - 1 scheduler warp walks the worker's share of the cost line and publishes segments (an item's range of tokens) ahead of the others.
+// The line counts token tiles up to the tile's last causal row, and kOverhead per item (queries, epilogue); items cut by a share's end are joined by the
+// combine kernel of the decode path.
+#include "splash_kv8.cuh"
+#include "splash_umma.cuh"
+
+namespace splash {
+
+namespace {
+
+using namespace kv8;
+using namespace umma;
+
+constexpr int kTileRows = 256, kTileTokens = 128;
+constexpr int kOverhead = 3;                       // cost of an item beside its tiles, in tiles of 128 tokens
+constexpr int kMinUnits = 4;                       // least cost of a worker's share
+constexpr int kWarpConvert = 8, kWarpMma = 12, kThreads = 32 * 14;      // (softmax 0 to 7, scheduler 13)
+constexpr int kNanBuffers = 8;
+
+enum { kEmptyItem = 1, kEndOfWork = 2 };
+
+struct alignas(16) Segment {
+    int request, row0, rows_all, pairs;
+    int m0, head, len, lo;             // lo, hi: tokens of the segment that the tile's last row sees
+    int hi, t0, tiles, slot;           // t0: first token of the first tile (a page's first)
+    int flags, pad[3];
+};
+
+enum {                                 // mbarriers
+    kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVEmpty = 6, kBarS = 8, kBarP = 10, kBarQ = 12, kBarO = 14, kBarScale = 16,
+    kBarSegFull = 20, kBarSegEmpty = 24, kNumBars = 28
+};
+
+template <int D>
+struct Layout {
+    static constexpr uint32_t kSlab = 128 * 128;                           // 128 rows of 64 fp16 values
+    static constexpr uint32_t kTile = kSlab * (D / 64);                    // 128 rows of D
+    static constexpr uint32_t kQ = 0;                                      // two halves of the row tile
+    static constexpr uint32_t kK = kQ + 2 * kTile, kV = kK + 2 * kTile;    // two stages each
+    static constexpr uint32_t kNan = kV + 2 * kTile;                       // [8][D] first token with a NaN in dimension d, per segment
+    static constexpr uint32_t kNanAny = kNan + kNanBuffers * 128 * 4;      // [8]
+    static constexpr uint32_t kScales = kNanAny + 32;                      // [4] tiles: two key scales, two value scales
+    static constexpr uint32_t kSegments = kScales + 64;                    // [4]
+    static constexpr uint32_t kBars = kSegments + 4 * sizeof(Segment);
+    static constexpr uint32_t kMisc = kBars + 8 * kNumBars;                // tensor memory address, abort flag
+    static constexpr uint32_t kBytes = kMisc + 16 + 1024;
+    static constexpr uint32_t kColS = 0, kColO = 256;                      // tensor memory: S (and P over it) 128 columns a half, O D columns a half
+};
+
+// fp16 operands, fp32 sums
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int b_mn_major) {
+    return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    umma_bf16(elected, d, a, b, idesc, accumulate);      // kind::f16: the operands' type is in the descriptor
+}
+// A from tensor memory: row m in lane m, two k to a column
+__device__ __forceinline__ void mma_ts(uint32_t elected, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+// ---- the cost line --------------------------------------------------------------------------------------------------------
+
+// Tokens that tile t of a request sees, and how many tiles of 128 from its first page on: its last row's range.
+struct TileRange { int hi, tiles; };
+__device__ __forceinline__ TileRange tile_range(const AttnParams &p, const Request &r, int t) {
+    const int last = (min((t + 1) * kTileRows, r.pairs) - 1) / p.group;
+    TileRange x;
+    x.hi = min(r.hi, r.len - r.rows_all + last + 1);
+    x.tiles = x.hi > r.lo ? (x.hi - r.lo / kPage * kPage + kTileTokens - 1) / kTileTokens : 0;
+    return x;
+}
+__device__ __forceinline__ int row_tiles(const AttnParams &p, const Request &r) {
+    return r.pairs < p.min_pairs || r.pairs > p.max_pairs ? 0 : (r.pairs + kTileRows - 1) / kTileRows;
+}
+// units of one key head of a request
+__device__ __forceinline__ int64_t head_units(const AttnParams &p, const Request &r) {
+    int64_t n = 0;
+    const int tiles = row_tiles(p, r);
+    for (int t = 0; t < tiles; ++t) n += kOverhead + tile_range(p, r, t).tiles;
+    return n;
+}
+
+struct Share { int64_t begin, end, total, u0; int i0, workers; };
+
+__device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
+    __shared__ int64_t sums[kThreads / 32];
+    __shared__ int64_t found_u;
+    __shared__ int found_i;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.B + kThreads - 1) / kThreads, i0 = min(tid * per, p.B), i1 = min(i0 + per, p.B);
+    int64_t mine = 0;
+    for (int i = i0; i < i1; ++i) mine += p.kv_heads * head_units(p, request(p, i));
+    int64_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += x;
+    }
+    if (lane == 31) sums[warp] = sum;
+    __syncthreads();
+    Share s;
+    s.total = 0;
+    int64_t before = sum - mine;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) before += sums[w];
+        s.total += sums[w];
+    }
+    // (every worker's share is worth a tile at least, so that each from an item's first to its last has a piece of it)
+    s.workers = (int)max((int64_t)1, min((int64_t)p.workers, s.total / kMinUnits));
+    s.begin = worker < s.workers ? s.total * worker / s.workers : s.total;
+    s.end = worker < s.workers ? s.total * (worker + 1) / s.workers : s.total;
+    if (s.begin < s.end && before <= s.begin && s.begin < before + mine) {
+        int64_t u = s.begin - before;
+        int i = i0;
+        for (; i < i1; ++i) {
+            const int64_t n = p.kv_heads * head_units(p, request(p, i));
+            if (u < n) break;
+            u -= n;
+        }
+        found_i = i;
+        found_u = u;
+    }
+    __syncthreads();
+    s.i0 = s.begin < s.end ? found_i : p.B;
+    s.u0 = s.begin < s.end ? found_u : 0;
+    return s;
+}
+
+// ---- roles ----------------------------------------------------------------------------------------------------------------
+
+struct Block {
+    const AttnParams &p;
+    uint8_t *smem;
+    uint32_t base, bars, tmem;         // shared-memory addresses; tensor memory
+    Ctx ctx;
+    __device__ __forceinline__ uint32_t bar(int id) const { return bars + 8u * (uint32_t)id; }
+};
+
+// Published segments by turns: take() waits for the next one, done() gives its place back (by every warp that takes).
+struct Segments {
+    const Block &b;
+    uint32_t offset, at = 0;
+    __device__ __forceinline__ bool take(Segment &s) {
+        if (!warp_wait(b.ctx, b.bar(kBarSegFull + (at & 3)), (at >> 2) & 1, kBarSegFull)) return false;
+        s = reinterpret_cast<const Segment *>(b.smem + offset)[at & 3];
+        return !(s.flags & kEndOfWork);
+    }
+    __device__ __forceinline__ void done(int lane) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.bar(kBarSegEmpty + (at & 3)));
+        ++at;
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void schedule(const Block &b, const Share &share, int worker, int lane) {
+    const AttnParams &p = b.p;
+    Segment *const ring = reinterpret_cast<Segment *>(b.smem + Layout<D>::kSegments);
+    uint32_t at = 0;
+    bool ok = true, has_cut = false;
+    auto publish = [&](const Segment &s) {
+        ok = warp_wait(b.ctx, b.bar(kBarSegEmpty + (at & 3)), ((at >> 2) & 1) ^ 1, kBarSegEmpty);
+        if (!ok) return;
+        if (lane == 0) {
+            ring[at & 3] = s;
+            mbar_arrive(b.bar(kBarSegFull + (at & 3)));
+        }
+        __syncwarp();
+        ++at;
+    };
+    int64_t line = share.begin;
+    int i = share.i0, head = 0, t = 0;
+    if (i < p.B) {
+        const Request r = request(p, i);
+        const int64_t per_head = head_units(p, r);
+        head = (int)(share.u0 / per_head);
+        int64_t u = share.u0 - head * per_head;
+        for (;; ++t) {
+            const int cost = kOverhead + tile_range(p, r, t).tiles;
+            if (u < cost) break;
+            u -= cost;
+        }
+        line -= u;                                   // where the item begins
+    }
+    while (ok && i < p.B && line < share.end) {
+        const Request r = request(p, i);
+        const int tiles = row_tiles(p, r);
+        for (; ok && head < p.kv_heads && line < share.end; ++head, t = 0)
+            for (; ok && t < tiles && line < share.end; ++t) {
+                const TileRange x = tile_range(p, r, t);
+                const int64_t first = line + kOverhead, end = first + x.tiles;
+                const bool mine = line >= share.begin;           // where items are not cut: the worker's that holds its first unit
+                const int64_t from = p.whole ? (mine ? first : end) : max(first, share.begin), to = p.whole ? end : min(end, share.end);
+                Segment s = {};
+                s.request = i; s.row0 = r.row0; s.rows_all = r.rows_all; s.pairs = r.pairs; s.m0 = t * kTileRows; s.head = head; s.len = r.len;
+                s.slot = -1;
+                if (from < to) {
+                    const int start = r.lo / kPage * kPage;
+                    s.tiles = (int)(to - from);
+                    s.t0 = start + (int)(from - first) * kTileTokens;
+                    s.lo = max(r.lo, s.t0);
+                    s.hi = to == end ? x.hi : s.t0 + s.tiles * kTileTokens;
+                    s.slot = from > first ? 2 * worker : to < end ? 2 * worker + 1 : -1;
+                    if (from == first && to < end) {
+                        if (lane == 0) {
+                            const int last = (int)((end * share.workers - 1) / share.total);     // the worker that holds the item's last unit
+                            p.cut[2 * worker] = make_int4(last - worker + 1, r.row0, r.pairs, s.m0);
+                            p.cut[2 * worker + 1] = make_int4(head, 0, 0, 0);
+                        }
+                        has_cut = true;
+                    }
+                    publish(s);
+                } else if (x.tiles == 0 && mine) {
+                    s.flags = kEmptyItem;
+                    publish(s);
+                }
+                line = end;
+            }
+        if (head == p.kv_heads) { ++i; head = 0; t = 0; }
+    }
+    if (ok) {
+        Segment s = {};
+        s.flags = kEndOfWork;
+        publish(s);
+    }
+    if (!has_cut && !p.whole && lane == 0) p.cut[2 * worker] = make_int4(0, 0, 0, 0);
+}
+
+template <int D>
+__device__ __forceinline__ void issue(const Block &b, int lane) {
+    using L = Layout<D>;
+    const uint32_t elected = elect_one(), tmem = uniform(b.tmem), base = uniform(b.base);
+    constexpr uint32_t kDescS = idesc_f16(128, 128, 0), kDescO = idesc_f16(128, D, 1);
+    Segments segments{b, L::kSegments};
+    Segment s;
+    uint32_t it = 0, seg = 0;
+    bool ok = true;
+    auto logits = [&](int half, uint32_t stage) {
+        const uint64_t q = make_desc(base + L::kQ + half * L::kTile, 16, 1024), k = make_desc(base + L::kK + stage * L::kTile, 16, 1024);
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) {
+            const uint32_t at = ((x >> 2) * L::kSlab + (x & 3) * 32) >> 4;
+            mma_ss(elected, tmem + L::kColS + half * 128, q + at, k + at, kDescS, x != 0);
+        }
+        if (elected) umma_commit(b.bar(kBarS + half));
+        __syncwarp();
+    };
+    while (ok && segments.take(s)) {
+        const int tiles = (int)uniform((uint32_t)s.tiles);
+        if (tiles > 0) {
+            for (int half = 0; half < 2 && ok; ++half) ok = warp_wait(b.ctx, b.bar(kBarQ + half), seg & 1, kBarQ);
+            if (ok) ok = warp_wait(b.ctx, b.bar(kBarKFull + (it & 1)), (it >> 1) & 1, kBarKFull);
+            if (!ok) break;
+            tcgen05_fence_after();
+            logits(0, it & 1);
+            logits(1, it & 1);
+            if (elected) umma_commit(b.bar(kBarKEmpty + (it & 1)));
+            __syncwarp();
+            for (int j = 0; ok && j < tiles; ++j, ++it) {
+                const uint32_t stage = it & 1, next = stage ^ 1;
+                ok = warp_wait(b.ctx, b.bar(kBarVFull + stage), (it >> 1) & 1, kBarVFull);
+                for (int half = 0; ok && half < 2; ++half) {
+                    ok = warp_wait(b.ctx, b.bar(kBarP + half), it & 1, kBarP);
+                    if (!ok) break;
+                    tcgen05_fence_after();
+                    const uint64_t v = make_desc(base + L::kV + stage * L::kTile, L::kSlab, 1024);
+#pragma unroll
+                    for (int x = 0; x < kTileTokens / 16; ++x)
+                        mma_ts(elected, tmem + L::kColO + half * D, tmem + L::kColS + half * 128 + x * 8, v + ((x * 2048) >> 4), kDescO, (uint32_t)j | (uint32_t)x);
+                    if (half == 1) {
+                        if (elected) umma_commit(b.bar(kBarVEmpty + stage));
+                        __syncwarp();
+                    }
+                    if (j + 1 < tiles) {
+                        if (half == 0) {
+                            ok = warp_wait(b.ctx, b.bar(kBarKFull + next), ((it + 1) >> 1) & 1, kBarKFull);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                        }
+                        logits(half, next);
+                        if (half == 1) {
+                            if (elected) umma_commit(b.bar(kBarKEmpty + next));
+                            __syncwarp();
+                        }
+                    } else {
+                        if (elected) umma_commit(b.bar(kBarO + half));
+                        __syncwarp();
+                    }
+                }
+            }
+            ++seg;
+        }
+        segments.done(lane);
+    }
+}
+
+// Codes of one tile's keys or values in registers on their way: 16 bytes of row `row + kStep * k`.
+template <int D>
+struct Codes {
+    static constexpr int kChunks = D / 16, kStep = 128 / kChunks, kRows = 128 / kStep;
+    uint4 w[kRows];
+    __device__ __forceinline__ void load(const uint8_t *page0, const uint8_t *page1, int t0, int lo, int hi, int tid) {
+        const int row = tid / kChunks, chunk = tid % kChunks;
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int r = row + kStep * k;
+            const uint8_t *const page = r < kPage ? page0 : page1;
+            w[k] = make_uint4(0, 0, 0, 0);
+            if (page != nullptr && t0 + r >= lo && t0 + r < hi) w[k] = *reinterpret_cast<const uint4 *>(page + (r & 63) * D + chunk * 16);
+        }
+    }
+    // as fp16 into a stage: rows of 64 values in the 128-byte swizzle, slabs of 128 rows
+    __device__ __forceinline__ void store(uint8_t *stage, int tid) const {
+        const int row = tid / kChunks, chunk = tid % kChunks;
+        uint8_t *const slab = stage + (chunk >> 2) * Layout<D>::kSlab;
+        const int unit = 2 * (chunk & 3), turn = chunk >> 2 & 1;         // lanes of the two slabs begin with different units: no bank twice
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const int r = row + kStep * k;
+            uint4 h[2];
+            to_f16x4(w[k].x, h[0].x, h[0].y); to_f16x4(w[k].y, h[0].z, h[0].w);
+            to_f16x4(w[k].z, h[1].x, h[1].y); to_f16x4(w[k].w, h[1].z, h[1].w);
+            *reinterpret_cast<uint4 *>(slab + r * 128 + (((unit + turn) ^ (r & 7)) << 4)) = turn ? h[1] : h[0];
+            *reinterpret_cast<uint4 *>(slab + r * 128 + (((unit + 1 - turn) ^ (r & 7)) << 4)) = turn ? h[0] : h[1];
+        }
+    }
+    // NaN codes become zeros; the first token with one is noted per dimension
+    __device__ __forceinline__ void take_out_nan(int *first, int *any, int t0, int tid) {
+        uint32_t found = 0;
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) found |= (u[q] & 0x7f7f7f7fu) + 0x01010101u;
+        }
+        if ((found & 0x80808080u) == 0) return;
+        const int row = tid / kChunks, chunk = tid % kChunks;
+        *any = 1;
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t at = (((u[q] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
+                u[q] &= ~(at * 0xffu);
+                for (int x = 0; x < 4; ++x)
+                    if (at >> (8 * x) & 1u) atomicMin(first + chunk * 16 + q * 4 + x, t0 + row + kStep * k);
+            }
+            w[k] = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void convert(const Block &b, const splash_kv8_cache &cache, int tid, int lane) {
+    using L = Layout<D>;
+    const AttnParams &p = b.p;
+    Segments segments{b, L::kSegments};
+    Segment s;
+    int *const nan = reinterpret_cast<int *>(b.smem + L::kNan), *const nan_any = reinterpret_cast<int *>(b.smem + L::kNanAny);
+    float *const scales = reinterpret_cast<float *>(b.smem + L::kScales);
+    uint32_t it = 0, seg = 0;
+    int j = 0, id[2] = {-1, -1};
+    // the next tile that has tokens: its pages (false: no more work)
+    auto pages = [&] {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int t = s.t0 + j * kTileTokens + k * kPage;
+            id[k] = t < s.hi ? load_l2(p.table + s.request * p.table_stride + t / kPage) : -1;
+            if (id[k] < 0 || id[k] >= p.num_pages) id[k] = -1;
+        }
+    };
+    auto open = [&]() -> bool {
+        for (;;) {
+            if (!segments.take(s)) return false;
+            if (s.tiles > 0) return true;
+            segments.done(lane);
+        }
+    };
+    auto page = [&](const void *pool, int64_t page_stride, int64_t head_stride, int k) {
+        return id[k] < 0 ? nullptr : static_cast<const uint8_t *>(pool) + id[k] * page_stride + s.head * head_stride;
+    };
+    Codes<D> keys, values;
+    float ks[2], vs[2];
+    auto fetch_keys = [&] {
+        keys.load(page(cache.k_pool, cache.k_page_stride, cache.k_head_stride, 0), page(cache.k_pool, cache.k_page_stride, cache.k_head_stride, 1),
+                  s.t0 + j * kTileTokens, s.lo, s.hi, tid);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            ks[k] = id[k] < 0 ? 0.f : p.k_scales[id[k] * p.k_scale_stride + s.head];
+            vs[k] = id[k] < 0 ? 0.f : p.v_scales[id[k] * p.v_scale_stride + s.head];
+        }
+    };
+    bool more = open();
+    if (more) { pages(); fetch_keys(); }
+    while (more) {
+        const uint32_t stage = it & 1, turn = it & 3;
+        int *const first = nan + (seg & (kNanBuffers - 1)) * 128, *const any = nan_any + (seg & (kNanBuffers - 1));
+        const int t0 = s.t0 + j * kTileTokens;
+        if (j == 0) {         // a warp is at most two tiles ahead of another, and the softmax warps at most two segments behind
+            nan[((seg + 2) & (kNanBuffers - 1)) * 128 + tid] = 0x7fffffff;
+            if (tid == 0) nan_any[(seg + 2) & (kNanBuffers - 1)] = 0;
+        }
+        values.load(page(cache.v_pool, cache.v_page_stride, cache.v_head_stride, 0), page(cache.v_pool, cache.v_page_stride, cache.v_head_stride, 1), t0, s.lo, s.hi, tid);
+        if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), ((it >> 1) & 1) ^ 1, kBarKEmpty)) return;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (!isfinite(vs[k])) {                      // every value of the page is NaN
+                const int token = max(s.lo, t0 + k * kPage);
+                if (tid < D) atomicMin(first + tid, token);
+                *any = 1;
+                vs[k] = 0.f;
+            }
+        if (tid == 0) {
+            scales[4 * turn] = ks[0]; scales[4 * turn + 1] = ks[1];
+            scales[4 * turn + 2] = vs[0]; scales[4 * turn + 3] = vs[1];
+            mbar_arrive(b.bar(kBarScale + turn));
+        }
+        keys.store(b.smem + L::kK + stage * L::kTile, tid);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.bar(kBarKFull + stage));
+        // the next tile's keys are on their way while this one's values are converted
+        const bool last = j + 1 == s.tiles;
+        if (last) {
+            segments.done(lane);
+            more = open();
+            j = 0;
+        } else {
+            ++j;
+        }
+        if (more) { pages(); fetch_keys(); }
+        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), ((it >> 1) & 1) ^ 1, kBarVEmpty)) return;
+        values.take_out_nan(first, any, t0, tid);
+        values.store(b.smem + L::kV + stage * L::kTile, tid);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b.bar(kBarVFull + stage));
+        ++it;
+        if (last) ++seg;
+    }
+}
+
+// 8 values of a row to out
+__device__ __forceinline__ void store8(const AttnParams &p, int64_t at, const float (&v)[8]) {
+    if (p.out_f32) {
+        float4 *const to = reinterpret_cast<float4 *>(static_cast<float *>(p.out) + at);
+        to[0] = make_float4(v[0], v[1], v[2], v[3]);
+        to[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.out) + at) =
+            p.q_bf16 ? make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]))
+                     : make_uint4(pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]), pack_f16x2(v[4], v[5]), pack_f16x2(v[6], v[7]));
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void soften(const Block &b, int half, int r /* row of the half */, int lane) {
+    using L = Layout<D>;
+    const AttnParams &p = b.p;
+    Segments segments{b, L::kSegments};
+    Segment s;
+    const uint32_t lanes = (uint32_t)(r & 96) << 16;
+    const uint32_t col_s = b.tmem + lanes + L::kColS + half * 128, col_o = b.tmem + lanes + L::kColO + half * D;
+    const float *const scales = reinterpret_cast<const float *>(b.smem + L::kScales);
+    uint32_t it = 0, seg = 0;
+    while (segments.take(s)) {
+        const int m = s.m0 + half * 128 + r, row = m / p.group, g = s.head * p.group + m - row * p.group;
+        const bool there = m < s.pairs;
+        const int64_t q_at = (s.row0 + (int64_t)row) * p.q_row + g * p.q_head, out_at = (s.row0 + (int64_t)row) * p.out_row + g * p.out_head;
+        if (s.flags & kEmptyItem) {
+            if (there) {
+                const float zero[8] = {};
+#pragma unroll
+                for (int d = 0; d < D; d += 8) store8(p, out_at + d, zero);
+                p.lse[(s.row0 + (int64_t)row) * p.lse_row + g] = -INFINITY;
+            }
+            segments.done(lane);
+            continue;
+        }
+        // ---- the row's queries, as fp16 with a power of two that brings the largest to [2^14, 2^15)
+        float back;
+        {
+            uint4 w[D / 8];
+            int most = 0;
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) {
+                w[k] = make_uint4(0, 0, 0, 0);
+                if (there) w[k] = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p.q) + q_at)[k];
+            }
+            // (the largest finite one, by its 16-bit pattern: patterns of finite values order like their sizes)
+            const int inf = p.q_bf16 ? 0x7f80 : 0x7c00;
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) {
+                const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int lo = u[x] & 0x7fff, hi = u[x] >> 16 & 0x7fff;
+                    if (lo < inf) most = max(most, lo);
+                    if (hi < inf) most = max(most, hi);
+                }
+            }
+            const float size = p.q_bf16 ? __int_as_float(most << 16) : __half2float(__ushort_as_half((unsigned short)most));
+            const int shift = most == 0 ? 0 : min(14 - ((__float_as_int(size) >> 23) - 127), 100);
+            const float factor = __int_as_float((shift + 127) << 23);
+            back = p.scale_log2 * __int_as_float((127 - shift) << 23);
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) {
+                const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                uint32_t h[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    float2 f;
+                    if (p.q_bf16) f = make_float2(__uint_as_float(u[x] << 16), __uint_as_float(u[x] & 0xffff0000u));
+                    else f = __half22float2(*reinterpret_cast<const __half2 *>(&u[x]));
+                    h[x] = pack_f16x2(f.x * factor, f.y * factor);
+                }
+                *reinterpret_cast<uint4 *>(b.smem + L::kQ + half * L::kTile + (k >> 3) * L::kSlab + r * 128 + (((k & 7) ^ (r & 7)) << 4)) =
+                    make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b.bar(kBarQ + half));
+        }
+        const int lim = there ? min(s.hi, s.len - s.rows_all + row + 1) : s.hi;
+        const int lim_min = __reduce_min_sync(0xffffffffu, lim);
+        float ref = kUnset, l = 0.f, unit = 0.f;
+        bool ok = true;
+        for (int j = 0; ok && j < s.tiles; ++j, ++it) {
+            const int t0 = s.t0 + j * kTileTokens;
+            ok = warp_wait(b.ctx, b.bar(kBarScale + (it & 3)), (it >> 2) & 1, kBarScale);
+            if (!ok) break;
+            const float4 sc = reinterpret_cast<const float4 *>(scales)[it & 3];
+            ok = warp_wait(b.ctx, b.bar(kBarS + half), it & 1, kBarS);
+            if (!ok) break;
+            tcgen05_fence_after();
+            // rescales the first `n` columns of O (D or none) and `done` columns of P
+            auto rescale = [&](float a, bool outputs, bool weights) {
+                if (outputs) {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        float v[16];
+                        tmem_ld16(col_o + c, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) v[x] *= a;
+                        tmem_st16(col_o + c, v);
+                    }
+                }
+                if (weights) {
+                    const __half2 h = __float2half2_rn(a);
+#pragma unroll 1
+                    for (int c = 0; c < 32; c += 16) {
+                        float v[16];
+                        uint32_t u[16];
+                        tmem_wait_st();
+                        tmem_ld16(col_s + c, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            const uint32_t bits = __float_as_uint(v[x]);
+                            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&bits), h);
+                            u[x] = *reinterpret_cast<const uint32_t *>(&y);
+                        }
+                        tmem_st16u(col_s + c, u);
+                    }
+                }
+            };
+            const float largest = fmaxf(fabsf(sc.z), fabsf(sc.w));
+            if (largest > unit) {
+                if (j > 0) rescale(__fdividef(unit, largest), true, false);
+                unit = largest;
+            }
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const float a = back * (h ? sc.y : sc.x), vsc = h ? sc.w : sc.z, f = vsc == unit ? 1.f : __fdividef(vsc, unit);
+                const int tb = t0 + h * kPage;
+                uint32_t v[64];
+                tmem_ld32(col_s + 64 * h, v);
+                tmem_ld32(col_s + 64 * h + 32, v + 32);
+                tmem_wait_ld();
+                const bool masked = tb < s.lo || tb + kPage > lim_min;
+                // visible columns of the page: [first, last)
+                const int first = masked ? s.lo - tb : 0, last = masked ? lim - tb : 64;
+                float most = -INFINITY;
+                if (masked) {
+#pragma unroll
+                    for (int x = 0; x < 64; ++x)
+                        if (x >= first && x < last) most = fmaxf(most, fmaf(__uint_as_float(v[x]), a, -ref));
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 64; ++x) most = fmaxf(most, fmaf(__uint_as_float(v[x]), a, -ref));
+                }
+                if (__any_sync(0xffffffffu, most > kLift + kSlack)) {
+                    // references are whole numbers, so that weights in tensor memory are rescaled without rounding
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int x = 0; x < 64; ++x)
+                        if (x >= first && x < last) top = fmaxf(top, __uint_as_float(v[x]) * a);
+                    top = floorf(top) - kLift;
+                    const bool grows = top > ref;
+                    const float factor = grows ? fast_exp2(ref - top) : 1.f;
+                    l *= factor;
+                    if (grows) ref = top;
+                    rescale(factor, j > 0, h == 1);
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t w[16];
+                    float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        float y0 = fmaf(__uint_as_float(v[32 * c + 2 * x]), a, -ref), y1 = fmaf(__uint_as_float(v[32 * c + 2 * x + 1]), a, -ref);
+                        if (masked) {
+                            const int at = 32 * c + 2 * x;
+                            if (at < first || at >= last) y0 = -INFINITY;
+                            if (at + 1 < first || at + 1 >= last) y1 = -INFINITY;
+                        }
+                        const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
+                        sum0 += p0;
+                        sum1 += p1;
+                        w[x] = pack_f16x2(p0 * f, p1 * f);
+                    }
+                    l += sum0 + sum1;
+                    tmem_st16u(col_s + 32 * h + 16 * c, w);
+                }
+            }
+            tmem_wait_st();
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b.bar(kBarP + half));
+        }
+        if (!ok) return;
+        // ---- epilogue
+        if (!warp_wait(b.ctx, b.bar(kBarO + half), seg & 1, kBarO)) return;
+        tcgen05_fence_after();
+        const float scale = l == 0.f ? 0.f : __fdividef(unit, l);
+        const float lse2 = l == 0.f ? -INFINITY : ref + __log2f(l);
+        const int *const nan = reinterpret_cast<const int *>(b.smem + L::kNan) + (seg & (kNanBuffers - 1)) * 128;
+        const bool nans = reinterpret_cast<const volatile int *>(b.smem + L::kNanAny)[seg & (kNanBuffers - 1)] != 0;
+        float *const part = p.part_out + ((int64_t)s.slot * kTileRows + half * 128 + r) * D;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16) {
+            float v[16];
+            tmem_ld16(col_o + c, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                v[x] *= scale;
+                if (nans && nan[c + x] < lim) v[x] = NAN;
+            }
+            if (there) {
+                if (s.slot < 0) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float u[8] = {v[8 * k], v[8 * k + 1], v[8 * k + 2], v[8 * k + 3], v[8 * k + 4], v[8 * k + 5], v[8 * k + 6], v[8 * k + 7]};
+                        store8(p, out_at + c + 8 * k, u);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) reinterpret_cast<float4 *>(part + c)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                }
+            }
+        }
+        if (there) {
+            if (s.slot < 0) p.lse[(s.row0 + (int64_t)row) * p.lse_row + g] = lse2 * kLn2;
+            else p.part_lse[s.slot * kTileRows + half * 128 + r] = lse2;
+        }
+        tcgen05_fence_before();
+        segments.done(lane);
+        ++seg;
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ splash_kv8_cache cache) {
+    using L = Layout<D>;
+    extern __shared__ uint8_t raw[];
+    uint8_t *const smem = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, worker = blockIdx.x;
+    volatile uint32_t *const misc = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
+    const uint32_t bars = smem_u32(smem + L::kBars);
+    if (tid == 0) {
+        for (int k = 0; k < 2; ++k) {
+            mbar_init(bars + 8 * (kBarKFull + k), 4); mbar_init(bars + 8 * (kBarKEmpty + k), 1);
+            mbar_init(bars + 8 * (kBarVFull + k), 4); mbar_init(bars + 8 * (kBarVEmpty + k), 1);
+            mbar_init(bars + 8 * (kBarS + k), 1); mbar_init(bars + 8 * (kBarP + k), 4);
+            mbar_init(bars + 8 * (kBarQ + k), 4); mbar_init(bars + 8 * (kBarO + k), 1);
+        }
+        for (int k = 0; k < 4; ++k) {
+            mbar_init(bars + 8 * (kBarScale + k), 1);
+            mbar_init(bars + 8 * (kBarSegFull + k), 1); mbar_init(bars + 8 * (kBarSegEmpty + k), 13);
+        }
+        misc[1] = 0;
+        for (int k = 0; k < kNanBuffers; ++k) reinterpret_cast<int *>(smem + L::kNanAny)[k] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int k = tid; k < kNanBuffers * 128; k += kThreads) reinterpret_cast<int *>(smem + L::kNan)[k] = 0x7fffffff;
+    if (warp == kWarpMma) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem + L::kMisc)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const Share share = plan(p, worker);
+    const Block b = {p, smem, smem_u32(smem), bars, misc[0], Ctx{misc + 1, p.status}};
+    if (warp < kWarpConvert) soften<D>(b, warp >> 2, tid & 127, lane);
+    else if (warp < kWarpMma) convert<D>(b, cache, tid - 32 * kWarpConvert, lane);
+    else if (warp == kWarpMma) issue<D>(b, lane);
+    else schedule<D>(b, share, worker, lane);
+    if (misc[1]) {
+        // a wait has given up: MMAs that were issued must be over before the tensor memory is
+        const unsigned long long since = global_timer_ns();
+        while (global_timer_ns() - since < 200000ull) __nanosleep(1000);
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == kWarpMma) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(misc[0]), "r"(512u) : "memory");
+    }
+}
+
+template <int D>
+cudaError_t launch_chunk(const AttnParams &p, const splash_kv8_cache &cache, cudaStream_t stream) {
+    static DeviceOnce once;
+    cudaError_t e = once.run([] { return cudaFuncSetAttribute(kv8_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Layout<D>::kBytes); });
+    if (e != cudaSuccess) return e;
+    e = launch_dependent(kv8_chunk_kernel<D>, dim3(p.workers), dim3(kThreads), Layout<D>::kBytes, stream, p, cache);
+    count_launch();
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_combine(const AttnParams &p, int D, int rows, int items, cudaStream_t stream);     // (of the decode path)
+
+int kv8_chunk_rows() { return kTileRows; }
+
+cudaError_t launch_kv8_chunk(const AttnParams &p, const splash_kv8_cache &cache, cudaStream_t stream) {
+    cudaError_t e = cache.head_dim == 128 ? launch_chunk<128>(p, cache, stream) : launch_chunk<64>(p, cache, stream);
+    if (e == cudaSuccess && !p.whole) e = launch_kv8_combine(p, cache.head_dim, kTileRows, p.workers, stream);
+    return e;
+}
+
+}  // namespace splash

@@ -35,8 +35,6 @@ constexpr int kConsumers = 4;                       // warps, 16 tokens of a pag
 constexpr int kThreads = 32 * (kConsumers + 1);
 constexpr int kOverhead = 2;                        // cost of an item beside its pages, in pages
 constexpr int kMinUnits = 2;                        // least cost of a worker's share
-constexpr float kLift = 7.f, kSlack = 8.f;          // weights are kept below 2^(kLift + kSlack) = 2^15
-constexpr float kUnset = -1e38f;                    // reference of a row that has seen no token: any logit is far above it
 
 enum { kFirst = 1, kLast = 2, kEmpty = 4, kEnd = 8, kEdge = 16, kCausal = 32 };
 
@@ -769,26 +767,37 @@ bool make_pool_map(CUtensorMap *map, const splash_kv8_cache &c, const void *pool
     return r == CUDA_SUCCESS;
 }
 
+// `items`: no more of them are cut
+template <int D, int kRows>
+cudaError_t launch_combine(const AttnParams &p, int items, cudaStream_t stream) {
+    static DeviceOnce once;
+    cudaError_t e = once.run([] {
+        // (an SM that had to change its shared memory between the two kernels would have to run empty first)
+        for (const auto kernel : {kv8_combine_kernel<D, kRows, 1>, kv8_combine_kernel<D, kRows, 4>}) {
+            const cudaError_t c = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+            if (c != cudaSuccess) return c;
+        }
+        return cudaSuccess;
+    });
+    if (e != cudaSuccess) return e;
+    e = p.workers / items >= 8 ? launch_dependent(kv8_combine_kernel<D, kRows, 4>, dim3(p.workers, kRows), dim3(128), 0, stream, p)
+                               : launch_dependent(kv8_combine_kernel<D, kRows, 1>, dim3(p.workers, kRows / 4), dim3(128), 0, stream, p);
+    count_launch();
+    return e;
+}
+
 template <int D, int NT>
 cudaError_t launch_decode(const AttnParams &p, int items, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
     using L = Layout<D, NT>;
     static DeviceOnce once;
     cudaError_t e = once.run([] {
-        // (an SM that had to change its shared memory between the two would have to run empty first)
-        for (const auto kernel : {kv8_combine_kernel<D, L::kRows, 1>, kv8_combine_kernel<D, L::kRows, 4>}) {
-            const cudaError_t c = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-            if (c != cudaSuccess) return c;
-        }
         return cudaFuncSetAttribute(kv8_decode_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
     });
     if (e != cudaSuccess) return e;
     e = launch_dependent(kv8_decode_kernel<D, NT>, dim3(p.workers), dim3(kThreads), L::kBytes, stream, p, k_map, v_map);
     count_launch();
     if (e != cudaSuccess || p.whole) return e;
-    e = p.workers / items >= 8 ? launch_dependent(kv8_combine_kernel<D, L::kRows, 4>, dim3(p.workers, L::kRows), dim3(128), 0, stream, p)
-                               : launch_dependent(kv8_combine_kernel<D, L::kRows, 1>, dim3(p.workers, L::kRows / 4), dim3(128), 0, stream, p);
-    count_launch();
-    return e;
+    return launch_combine<D, L::kRows>(p, items, stream);
 }
 
 }  // namespace
@@ -804,8 +813,14 @@ bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v
     return make_pool_map(k_map, c, c.k_pool, c.k_page_stride, c.k_head_stride) && make_pool_map(v_map, c, c.v_pool, c.v_page_stride, c.v_head_stride);
 }
 
+// of the kernel for many rows
+cudaError_t launch_kv8_combine(const AttnParams &p, int D, int rows, int items, cudaStream_t stream) {
+    if (rows != 256) return cudaErrorInvalidValue;
+    return D == 128 ? launch_combine<128, 256>(p, items, stream) : launch_combine<64, 256>(p, items, stream);
+}
+
 cudaError_t launch_kv8_decode(const AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
-    const int64_t tiles = ((int64_t)p.max_rows * p.group + rows - 1) / rows, all = tiles * p.kv_heads * p.B;
+    const int64_t pairs = (int64_t)p.max_rows * p.group, tiles = ((pairs < p.max_pairs ? pairs : p.max_pairs) + rows - 1) / rows, all = tiles * p.kv_heads * p.B;
     const int items = (int)(all < 0x7fffffff ? all : 0x7fffffff);        // at most
     auto of = [&](auto d) {
         constexpr int kD = decltype(d)::value;

@@ -29,7 +29,7 @@ def attend(cache, q, rows, dtype="bf16", scale=None, kv=None, out_dtype=None, wi
         kw["kv_begin"], kw["kv_end"] = (None if a is None else torch.tensor(a, dtype=torch.int32, device="cuda") for a in kv)
     if out_dtype == "fp32":
         kw["out"] = torch.full(q.shape, 7.0, device="cuda")
-    ws = torch.empty(1 << 25, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
     out, lse = B.splash_kv8_attention(q.cuda() if q.device.type == "cpu" else q, *tensors, softmax_scale=scale, workspace=ws, **kw)
     torch.cuda.synchronize()
     assert B.splash_workspace_status(ws)[0] == 0
