@@ -37,9 +37,17 @@ struct alignas(16) Segment {
     int flags, pad[3];
 };
 
+// A tile of 128 tokens for the converters: its two pages' rows of the key head (NULL: none, zeros) and their scales.
+struct alignas(16) Tile {
+    const uint8_t *keys[2], *values[2];
+    float k_scale[2], v_scale[2];
+    int t0, lo, hi, flags;
+};
+enum { kTileEdge = 1 /* not all rows see all its tokens */, kTileLast = 2 /* of its segment */, kTileEnd = 4 };
+
 enum {                                 // mbarriers
     kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVEmpty = 6, kBarS = 8, kBarP = 10, kBarQ = 12, kBarO = 14, kBarScale = 16,
-    kBarSegFull = 20, kBarSegEmpty = 24, kNumBars = 28
+    kBarSegFull = 20, kBarSegEmpty = 24, kBarTileFull = 28, kBarTileEmpty = 32, kNumBars = 36
 };
 
 template <int D>
@@ -52,7 +60,8 @@ struct Layout {
     static constexpr uint32_t kNanAny = kNan + kNanBuffers * 128 * 4;      // [8]
     static constexpr uint32_t kScales = kNanAny + 32;                      // [4] tiles: two key scales, two value scales
     static constexpr uint32_t kSegments = kScales + 64;                    // [4]
-    static constexpr uint32_t kBars = kSegments + 4 * sizeof(Segment);
+    static constexpr uint32_t kTiles = kSegments + 4 * sizeof(Segment);    // [4]
+    static constexpr uint32_t kBars = kTiles + 4 * sizeof(Tile);
     static constexpr uint32_t kMisc = kBars + 8 * kNumBars;                // tensor memory address, abort flag
     static constexpr uint32_t kBytes = kMisc + 16 + 1024;
     static constexpr uint32_t kColS = 0, kColO = 256;                      // tensor memory: S (and P over it) 128 columns a half, O D columns a half
@@ -85,6 +94,14 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t *r) {
           "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
           "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr) : "memory");
+}
+// until such a load has arrived: nothing is done with its registers before
+__device__ __forceinline__ void tmem_wait_ld32(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+          "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]),
+          "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+        :: "memory");
 }
 __device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
@@ -175,10 +192,10 @@ struct Block {
 struct Segments {
     const Block &b;
     uint32_t offset, at = 0;
-    __device__ __forceinline__ bool take(Segment &s) {
-        if (!warp_wait(b.ctx, b.bar(kBarSegFull + (at & 3)), (at >> 2) & 1, kBarSegFull)) return false;
-        s = reinterpret_cast<const Segment *>(b.smem + offset)[at & 3];
-        return !(s.flags & kEndOfWork);
+    __device__ __forceinline__ const Segment *take() {
+        if (!warp_wait(b.ctx, b.bar(kBarSegFull + (at & 3)), (at >> 2) & 1, kBarSegFull)) return nullptr;
+        const Segment *const s = reinterpret_cast<const Segment *>(b.smem + offset) + (at & 3);
+        return s->flags & kEndOfWork ? nullptr : s;
     }
     __device__ __forceinline__ void done(int lane) {
         __syncwarp();
@@ -188,8 +205,10 @@ struct Segments {
 };
 
 template <int D>
-__device__ __forceinline__ void schedule(const Block &b, const Share &share, int worker, int lane) {
+__device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache &cache, const Share &share, int worker, int lane) {
     const AttnParams &p = b.p;
+    Tile *const tiles_ring = reinterpret_cast<Tile *>(b.smem + Layout<D>::kTiles);
+    uint32_t tile_at = 0;
     Segment *const ring = reinterpret_cast<Segment *>(b.smem + Layout<D>::kSegments);
     uint32_t at = 0;
     bool ok = true, has_cut = false;
@@ -202,6 +221,38 @@ __device__ __forceinline__ void schedule(const Block &b, const Share &share, int
         }
         __syncwarp();
         ++at;
+    };
+    // the segment's tiles: a lane each finds its pages and scales
+    auto publish_tiles = [&](const Segment &s) {
+        for (int j0 = 0; ok && j0 < s.tiles; j0 += 32) {
+            const int j = j0 + lane;
+            Tile t = {};
+            t.t0 = s.t0 + j * kTileTokens; t.lo = s.lo; t.hi = s.hi;
+            if (j < s.tiles) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = t.t0 + k * kPage, id = at < s.hi ? load_l2(p.table + s.request * p.table_stride + at / kPage) : -1;
+                    if (id >= 0 && id < p.num_pages) {
+                        t.keys[k] = static_cast<const uint8_t *>(cache.k_pool) + id * cache.k_page_stride + s.head * cache.k_head_stride;
+                        t.values[k] = static_cast<const uint8_t *>(cache.v_pool) + id * cache.v_page_stride + s.head * cache.v_head_stride;
+                        t.k_scale[k] = p.k_scales[id * p.k_scale_stride + s.head];
+                        t.v_scale[k] = p.v_scales[id * p.v_scale_stride + s.head];
+                    }
+                }
+                if (t.t0 < s.lo || t.t0 + kTileTokens > min(s.hi, s.len - s.rows_all + s.m0 / p.group + 1)) t.flags |= kTileEdge;
+                if (j + 1 == s.tiles) t.flags |= kTileLast;
+            }
+            for (int k = 0; ok && k < 32 && j0 + k < s.tiles; ++k) {
+                ok = warp_wait(b.ctx, b.bar(kBarTileEmpty + (tile_at & 3)), ((tile_at >> 2) & 1) ^ 1, kBarTileEmpty);
+                if (!ok) break;
+                if (lane == k) {
+                    tiles_ring[tile_at & 3] = t;
+                    mbar_arrive(b.bar(kBarTileFull + (tile_at & 3)));
+                }
+                __syncwarp();
+                ++tile_at;
+            }
+        }
     };
     int64_t line = share.begin;
     int i = share.i0, head = 0, t = 0;
@@ -245,6 +296,7 @@ __device__ __forceinline__ void schedule(const Block &b, const Share &share, int
                         has_cut = true;
                     }
                     publish(s);
+                    publish_tiles(s);
                 } else if (x.tiles == 0 && mine) {
                     s.flags = kEmptyItem;
                     publish(s);
@@ -257,17 +309,23 @@ __device__ __forceinline__ void schedule(const Block &b, const Share &share, int
         Segment s = {};
         s.flags = kEndOfWork;
         publish(s);
+        if (ok) ok = warp_wait(b.ctx, b.bar(kBarTileEmpty + (tile_at & 3)), ((tile_at >> 2) & 1) ^ 1, kBarTileEmpty);
+        if (ok && lane == 0) {
+            tiles_ring[tile_at & 3].flags = kTileEnd;
+            mbar_arrive(b.bar(kBarTileFull + (tile_at & 3)));
+        }
     }
     if (!has_cut && !p.whole && lane == 0) p.cut[2 * worker] = make_int4(0, 0, 0, 0);
 }
 
+// (What the converters have written is handed over to the async proxy here, behind the wait for them: a fence of theirs would wait for their loads of
+// the next tile, which they have under way all the time.)
 template <int D>
 __device__ __forceinline__ void issue(const Block &b, int lane) {
     using L = Layout<D>;
     const uint32_t elected = elect_one(), tmem = uniform(b.tmem), base = uniform(b.base);
     constexpr uint32_t kDescS = idesc_f16(128, 128, 0), kDescO = idesc_f16(128, D, 1);
     Segments segments{b, L::kSegments};
-    Segment s;
     uint32_t it = 0, seg = 0;
     bool ok = true;
     auto logits = [&](int half, uint32_t stage) {
@@ -280,12 +338,15 @@ __device__ __forceinline__ void issue(const Block &b, int lane) {
         if (elected) umma_commit(b.bar(kBarS + half));
         __syncwarp();
     };
-    while (ok && segments.take(s)) {
-        const int tiles = (int)uniform((uint32_t)s.tiles);
+    while (ok) {
+        const Segment *const s = segments.take();
+        if (s == nullptr) break;
+        const int tiles = (int)uniform((uint32_t)s->tiles);
         if (tiles > 0) {
             for (int half = 0; half < 2 && ok; ++half) ok = warp_wait(b.ctx, b.bar(kBarQ + half), seg & 1, kBarQ);
             if (ok) ok = warp_wait(b.ctx, b.bar(kBarKFull + (it & 1)), (it >> 1) & 1, kBarKFull);
             if (!ok) break;
+            fence_proxy_async();
             tcgen05_fence_after();
             logits(0, it & 1);
             logits(1, it & 1);
@@ -294,6 +355,7 @@ __device__ __forceinline__ void issue(const Block &b, int lane) {
             for (int j = 0; ok && j < tiles; ++j, ++it) {
                 const uint32_t stage = it & 1, next = stage ^ 1;
                 ok = warp_wait(b.ctx, b.bar(kBarVFull + stage), (it >> 1) & 1, kBarVFull);
+                fence_proxy_async();
                 for (int half = 0; ok && half < 2; ++half) {
                     ok = warp_wait(b.ctx, b.bar(kBarP + half), it & 1, kBarP);
                     if (!ok) break;
@@ -310,6 +372,7 @@ __device__ __forceinline__ void issue(const Block &b, int lane) {
                         if (half == 0) {
                             ok = warp_wait(b.ctx, b.bar(kBarKFull + next), ((it + 1) >> 1) & 1, kBarKFull);
                             if (!ok) break;
+                            fence_proxy_async();
                             tcgen05_fence_after();
                         }
                         logits(half, next);
@@ -329,151 +392,217 @@ __device__ __forceinline__ void issue(const Block &b, int lane) {
     }
 }
 
-// Codes of one tile's keys or values in registers on their way: 16 bytes of row `row + kStep * k`.
+// Codes of one tile's keys or values in registers on their way.  A lane has 16 bytes of rows 32 k + row in each slab of 64 dimensions, row = 8 warp +
+// lane / 4: row mod 8, and with it the swizzle, is the same for all of them, and eight lanes' stores (four chunks of an even and of an odd
+// row) meet no bank twice.
 template <int D>
 struct Codes {
-    static constexpr int kChunks = D / 16, kStep = 128 / kChunks, kRows = 128 / kStep;
-    uint4 w[kRows];
-    __device__ __forceinline__ void load(const uint8_t *page0, const uint8_t *page1, int t0, int lo, int hi, int tid) {
-        const int row = tid / kChunks, chunk = tid % kChunks;
+    static constexpr int kSlabs = D / 64, kUnits = 4 * kSlabs;
+    uint4 w[kUnits];
+    static __device__ __forceinline__ int row_of(int tid) { return (tid >> 5) * 8 + (tid >> 2 & 7); }
+    // page k: the pages of the tile's first and last 64 tokens, NULL: zeros; edge: tokens outside [lo, hi) are zeros too
+    __device__ __forceinline__ void load(const uint8_t *page0, const uint8_t *page1, bool edge, int t0, int lo, int hi, int tid) {
+        const int row = row_of(tid), at = row * D + (tid & 3) * 16;
+        if (!edge && page0 != nullptr && page1 != nullptr) {
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            const int r = row + kStep * k;
-            const uint8_t *const page = r < kPage ? page0 : page1;
-            w[k] = make_uint4(0, 0, 0, 0);
-            if (page != nullptr && t0 + r >= lo && t0 + r < hi) w[k] = *reinterpret_cast<const uint4 *>(page + (r & 63) * D + chunk * 16);
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int x = 0; x < kSlabs; ++x) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>((k < 2 ? page0 : page1) + at + (k & 1) * 32 * D + x * 64);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint8_t *const page = k < 2 ? page0 : page1;
+            const int t = t0 + 32 * k + row;
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x) {
+                w[k * kSlabs + x] = make_uint4(0, 0, 0, 0);
+                if (page != nullptr && t >= lo && t < hi) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>(page + at + (k & 1) * 32 * D + x * 64);
+            }
         }
     }
     // as fp16 into a stage: rows of 64 values in the 128-byte swizzle, slabs of 128 rows
     __device__ __forceinline__ void store(uint8_t *stage, int tid) const {
-        const int row = tid / kChunks, chunk = tid % kChunks;
-        uint8_t *const slab = stage + (chunk >> 2) * Layout<D>::kSlab;
-        const int unit = 2 * (chunk & 3), turn = chunk >> 2 & 1;         // lanes of the two slabs begin with different units: no bank twice
+        const int row = row_of(tid), unit = 2 * (tid & 3);
+        uint8_t *const even = stage + row * 128 + ((unit ^ (row & 7)) << 4), *const odd = stage + row * 128 + (((unit + 1) ^ (row & 7)) << 4);
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            const int r = row + kStep * k;
-            uint4 h[2];
-            to_f16x4(w[k].x, h[0].x, h[0].y); to_f16x4(w[k].y, h[0].z, h[0].w);
-            to_f16x4(w[k].z, h[1].x, h[1].y); to_f16x4(w[k].w, h[1].z, h[1].w);
-            *reinterpret_cast<uint4 *>(slab + r * 128 + (((unit + turn) ^ (r & 7)) << 4)) = turn ? h[1] : h[0];
-            *reinterpret_cast<uint4 *>(slab + r * 128 + (((unit + 1 - turn) ^ (r & 7)) << 4)) = turn ? h[0] : h[1];
-        }
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int x = 0; x < kSlabs; ++x) {
+                const uint4 c = w[k * kSlabs + x];
+                uint4 h;
+                to_f16x4(c.x, h.x, h.y);
+                to_f16x4(c.y, h.z, h.w);
+                *reinterpret_cast<uint4 *>(even + x * Layout<D>::kSlab + k * 32 * 128) = h;
+                to_f16x4(c.z, h.x, h.y);
+                to_f16x4(c.w, h.z, h.w);
+                *reinterpret_cast<uint4 *>(odd + x * Layout<D>::kSlab + k * 32 * 128) = h;
+            }
     }
     // NaN codes become zeros; the first token with one is noted per dimension
     __device__ __forceinline__ void take_out_nan(int *first, int *any, int t0, int tid) {
         uint32_t found = 0;
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        for (int k = 0; k < kUnits; ++k)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) found |= (u[q] & 0x7f7f7f7fu) + 0x01010101u;
-        }
+            for (const uint32_t u : {w[k].x, w[k].y, w[k].z, w[k].w}) found |= (u & 0x7f7f7f7fu) + 0x01010101u;
         if ((found & 0x80808080u) == 0) return;
-        const int row = tid / kChunks, chunk = tid % kChunks;
         *any = 1;
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t at = (((u[q] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
-                u[q] &= ~(at * 0xffu);
-                for (int x = 0; x < 4; ++x)
-                    if (at >> (8 * x) & 1u) atomicMin(first + chunk * 16 + q * 4 + x, t0 + row + kStep * k);
+            for (int x = 0; x < kSlabs; ++x) {
+                const uint4 c = w[k * kSlabs + x];
+                uint32_t u[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t at = (((u[q] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
+                    u[q] &= ~(at * 0xffu);
+                    for (int i = 0; i < 4; ++i)
+                        if (at >> (8 * i) & 1u) atomicMin(first + x * 64 + (tid & 3) * 16 + q * 4 + i, t0 + 32 * k + row_of(tid));
+                }
+                w[k * kSlabs + x] = make_uint4(u[0], u[1], u[2], u[3]);
             }
-            w[k] = make_uint4(u[0], u[1], u[2], u[3]);
-        }
     }
 };
 
 template <int D>
-__device__ __forceinline__ void convert(const Block &b, const splash_kv8_cache &cache, int tid, int lane) {
+__device__ __forceinline__ void convert(const Block &b, int tid, int lane) {
     using L = Layout<D>;
-    const AttnParams &p = b.p;
-    Segments segments{b, L::kSegments};
-    Segment s;
     int *const nan = reinterpret_cast<int *>(b.smem + L::kNan), *const nan_any = reinterpret_cast<int *>(b.smem + L::kNanAny);
     float *const scales = reinterpret_cast<float *>(b.smem + L::kScales);
-    uint32_t it = 0, seg = 0;
-    int j = 0, id[2] = {-1, -1};
-    // the next tile that has tokens: its pages (false: no more work)
-    auto pages = [&] {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int t = s.t0 + j * kTileTokens + k * kPage;
-            id[k] = t < s.hi ? load_l2(p.table + s.request * p.table_stride + t / kPage) : -1;
-            if (id[k] < 0 || id[k] >= p.num_pages) id[k] = -1;
-        }
-    };
-    auto open = [&]() -> bool {
-        for (;;) {
-            if (!segments.take(s)) return false;
-            if (s.tiles > 0) return true;
-            segments.done(lane);
-        }
-    };
-    auto page = [&](const void *pool, int64_t page_stride, int64_t head_stride, int k) {
-        return id[k] < 0 ? nullptr : static_cast<const uint8_t *>(pool) + id[k] * page_stride + s.head * head_stride;
-    };
+    const Tile *const ring = reinterpret_cast<const Tile *>(b.smem + L::kTiles);
+    // codes are fetched a tile ahead, keys behind the conversion of keys and values behind that of values
     Codes<D> keys, values;
-    float ks[2], vs[2];
-    auto fetch_keys = [&] {
-        keys.load(page(cache.k_pool, cache.k_page_stride, cache.k_head_stride, 0), page(cache.k_pool, cache.k_page_stride, cache.k_head_stride, 1),
-                  s.t0 + j * kTileTokens, s.lo, s.hi, tid);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            ks[k] = id[k] < 0 ? 0.f : p.k_scales[id[k] * p.k_scale_stride + s.head];
-            vs[k] = id[k] < 0 ? 0.f : p.v_scales[id[k] * p.v_scale_stride + s.head];
-        }
-    };
-    bool more = open();
-    if (more) { pages(); fetch_keys(); }
-    while (more) {
+    uint32_t it = 0, seg = 0;
+    bool begins = true;
+    if (!warp_wait(b.ctx, b.bar(kBarTileFull), 0, kBarTileFull)) return;
+    bool there = !(ring[0].flags & kTileEnd);
+    auto fetch_keys = [&](const Tile &t) { keys.load(t.keys[0], t.keys[1], t.flags & kTileEdge, t.t0, t.lo, t.hi, tid); };
+    auto fetch_values = [&](const Tile &t) { values.load(t.values[0], t.values[1], t.flags & kTileEdge, t.t0, t.lo, t.hi, tid); };
+    if (there) { fetch_keys(ring[0]); fetch_values(ring[0]); }
+    while (there) {
         const uint32_t stage = it & 1, turn = it & 3;
+        const Tile &now = ring[turn], &next = ring[(it + 1) & 3];
+        const int flags = now.flags;
         int *const first = nan + (seg & (kNanBuffers - 1)) * 128, *const any = nan_any + (seg & (kNanBuffers - 1));
-        const int t0 = s.t0 + j * kTileTokens;
-        if (j == 0) {         // a warp is at most two tiles ahead of another, and the softmax warps at most two segments behind
+        if (begins) {         // a warp is at most two tiles ahead of another, and the softmax warps at most two segments behind
             nan[((seg + 2) & (kNanBuffers - 1)) * 128 + tid] = 0x7fffffff;
             if (tid == 0) nan_any[(seg + 2) & (kNanBuffers - 1)] = 0;
         }
-        values.load(page(cache.v_pool, cache.v_page_stride, cache.v_head_stride, 0), page(cache.v_pool, cache.v_page_stride, cache.v_head_stride, 1), t0, s.lo, s.hi, tid);
         if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), ((it >> 1) & 1) ^ 1, kBarKEmpty)) return;
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (!isfinite(vs[k])) {                      // every value of the page is NaN
-                const int token = max(s.lo, t0 + k * kPage);
-                if (tid < D) atomicMin(first + tid, token);
-                *any = 1;
-                vs[k] = 0.f;
-            }
-        if (tid == 0) {
-            scales[4 * turn] = ks[0]; scales[4 * turn + 1] = ks[1];
-            scales[4 * turn + 2] = vs[0]; scales[4 * turn + 3] = vs[1];
-            mbar_arrive(b.bar(kBarScale + turn));
-        }
         keys.store(b.smem + L::kK + stage * L::kTile, tid);
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b.bar(kBarKFull + stage));
-        // the next tile's keys are on their way while this one's values are converted
-        const bool last = j + 1 == s.tiles;
-        if (last) {
-            segments.done(lane);
-            more = open();
-            j = 0;
-        } else {
-            ++j;
+        if (flags & kTileEdge) {
+            for (int k = 0; k < 2; ++k)
+                if (!isfinite(now.v_scale[k])) {         // every value of the page is NaN, for the rows that see a token of it
+                    if (tid < D) atomicMin(first + tid, max(now.lo, now.t0 + k * kPage));
+                    *any = 1;
+                }
         }
-        if (more) { pages(); fetch_keys(); }
-        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), ((it >> 1) & 1) ^ 1, kBarVEmpty)) return;
-        values.take_out_nan(first, any, t0, tid);
-        values.store(b.smem + L::kV + stage * L::kTile, tid);
-        fence_proxy_async();
+        if (tid < 4) {
+            float x = tid < 2 ? now.k_scale[tid] : now.v_scale[tid - 2];
+            if (tid >= 2 && !isfinite(x)) x = flags & kTileEdge ? 0.f : NAN;
+            scales[4 * turn + tid] = x;
+        }
         __syncwarp();
-        if (lane == 0) mbar_arrive(b.bar(kBarVFull + stage));
+        if (tid == 0) mbar_arrive(b.bar(kBarScale + turn));
+        if (lane == 0) mbar_arrive(b.bar(kBarKFull + stage));
+        if (!warp_wait(b.ctx, b.bar(kBarTileFull + ((it + 1) & 3)), ((it + 1) >> 2) & 1, kBarTileFull)) return;
+        there = !(next.flags & kTileEnd);
+        if (there) fetch_keys(next);
+        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), ((it >> 1) & 1) ^ 1, kBarVEmpty)) return;
+        if (flags & kTileEdge) values.take_out_nan(first, any, now.t0, tid);      // (0 * NaN must not reach rows that do not see it)
+        values.store(b.smem + L::kV + stage * L::kTile, tid);
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(b.bar(kBarVFull + stage));
+            mbar_arrive(b.bar(kBarTileEmpty + turn));
+        }
+        if (there) fetch_values(next);
         ++it;
-        if (last) ++seg;
+        begins = flags & kTileLast;
+        if (begins) ++seg;
     }
+}
+
+// two fp32 values at a time
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// The warp's rows of O (`cols` columns) and of the weights so far (`weights` columns of two fp16 over S), times a factor per row.
+__device__ __noinline__ void rescale(uint32_t col_o, int cols, uint32_t col_p, int weights, float a) {
+    for (int c = 0; c < cols; c += 16) {
+        float v[16];
+        tmem_ld16(col_o + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) v[x] *= a;
+        tmem_st16(col_o + c, v);
+    }
+    const __half2 h = __float2half2_rn(a);
+    tmem_wait_st();
+    for (int c = 0; c < weights; c += 16) {
+        float v[16];
+        uint32_t u[16];
+        tmem_ld16(col_p + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const uint32_t bits = __float_as_uint(v[x]);
+            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&bits), h);
+            u[x] = *reinterpret_cast<const uint32_t *>(&y);
+        }
+        tmem_st16u(col_p + c, u);
+    }
+}
+
+// The largest of 32 sums, times their factor.
+__device__ __noinline__ float largest_logit(uint32_t col, float a) {
+    float top = -INFINITY;
+    for (int c = 0; c < 32; c += 16) {
+        float v[16];
+        tmem_ld16(col + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) top = fmaxf(top, v[x] * a);
+    }
+    return top;
+}
+
+// The sums of a page's tokens that a row does not see (columns outside [first, last)) become such that their logits are -inf whatever the factor
+// (which is changed where no such sum exists); those that it sees become NaN if the factor is.
+__device__ __noinline__ float hide(uint32_t col, int first, int last, float a) {
+    const bool nan = !(a == a);
+    const float hidden = a < 0.f ? INFINITY : -INFINITY;
+    for (int c = 0; c < 64; c += 16) {
+        float v[16];
+        tmem_ld16(col + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) v[x] = c + x < first || c + x >= last ? hidden : nan ? NAN : v[x];
+        tmem_st16(col + c, v);
+    }
+    tmem_wait_st();
+    return nan ? 1.f : a == 0.f ? 1e-30f : a;
 }
 
 // 8 values of a row to out
@@ -494,12 +623,14 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
     using L = Layout<D>;
     const AttnParams &p = b.p;
     Segments segments{b, L::kSegments};
-    Segment s;
     const uint32_t lanes = (uint32_t)(r & 96) << 16;
     const uint32_t col_s = b.tmem + lanes + L::kColS + half * 128, col_o = b.tmem + lanes + L::kColO + half * D;
     const float *const scales = reinterpret_cast<const float *>(b.smem + L::kScales);
     uint32_t it = 0, seg = 0;
-    while (segments.take(s)) {
+    for (;;) {
+        const Segment *const at = segments.take();
+        if (at == nullptr) break;
+        const Segment &s = *at;
         const int m = s.m0 + half * 128 + r, row = m / p.group, g = s.head * p.group + m - row * p.group;
         const bool there = m < s.pairs;
         const int64_t q_at = (s.row0 + (int64_t)row) * p.q_row + g * p.q_head, out_at = (s.row0 + (int64_t)row) * p.out_row + g * p.out_head;
@@ -559,107 +690,84 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
         }
         const int lim = there ? min(s.hi, s.len - s.rows_all + row + 1) : s.hi;
         const int lim_min = __reduce_min_sync(0xffffffffu, lim);
+        const int lo = s.lo, tiles = s.tiles, start = s.t0;
         float ref = kUnset, l = 0.f, unit = 0.f;
         bool ok = true;
-        for (int j = 0; ok && j < s.tiles; ++j, ++it) {
-            const int t0 = s.t0 + j * kTileTokens;
+        for (int j = 0; ok && j < tiles; ++j, ++it) {
+            const int t0 = start + j * kTileTokens;
             ok = warp_wait(b.ctx, b.bar(kBarScale + (it & 3)), (it >> 2) & 1, kBarScale);
             if (!ok) break;
             const float4 sc = reinterpret_cast<const float4 *>(scales)[it & 3];
             ok = warp_wait(b.ctx, b.bar(kBarS + half), it & 1, kBarS);
             if (!ok) break;
             tcgen05_fence_after();
-            // rescales the first `n` columns of O (D or none) and `done` columns of P
-            auto rescale = [&](float a, bool outputs, bool weights) {
-                if (outputs) {
-#pragma unroll 1
-                    for (int c = 0; c < D; c += 16) {
-                        float v[16];
-                        tmem_ld16(col_o + c, v);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) v[x] *= a;
-                        tmem_st16(col_o + c, v);
-                    }
-                }
-                if (weights) {
-                    const __half2 h = __float2half2_rn(a);
-#pragma unroll 1
-                    for (int c = 0; c < 32; c += 16) {
-                        float v[16];
-                        uint32_t u[16];
-                        tmem_wait_st();
-                        tmem_ld16(col_s + c, v);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            const uint32_t bits = __float_as_uint(v[x]);
-                            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&bits), h);
-                            u[x] = *reinterpret_cast<const uint32_t *>(&y);
-                        }
-                        tmem_st16u(col_s + c, u);
-                    }
-                }
-            };
             const float largest = fmaxf(fabsf(sc.z), fabsf(sc.w));
             if (largest > unit) {
-                if (j > 0) rescale(__fdividef(unit, largest), true, false);
+                if (j > 0) rescale(col_o, D, col_s, 0, __fdividef(unit, largest));
                 unit = largest;
             }
-#pragma unroll 1
+            float a[2] = {back * sc.x, back * sc.y}, f[2];
+#pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float a = back * (h ? sc.y : sc.x), vsc = h ? sc.w : sc.z, f = vsc == unit ? 1.f : __fdividef(vsc, unit);
+                const float vsc = h ? sc.w : sc.z;
+                f[h] = vsc == unit ? 1.f : __fdividef(vsc, unit);
                 const int tb = t0 + h * kPage;
-                uint32_t v[64];
-                tmem_ld32(col_s + 64 * h, v);
-                tmem_ld32(col_s + 64 * h + 32, v + 32);
-                tmem_wait_ld();
-                const bool masked = tb < s.lo || tb + kPage > lim_min;
-                // visible columns of the page: [first, last)
-                const int first = masked ? s.lo - tb : 0, last = masked ? lim - tb : 64;
-                float most = -INFINITY;
-                if (masked) {
+                if (tb < lo || tb + kPage > lim_min) a[h] = hide(col_s + 64 * h, lo - tb, lim - tb, a[h]);
+            }
+            uint64_t sum[2] = {0, 0};
+            // 32 columns: y = x - ref, p = 2^y, to where columns that are done with lie
+            auto weigh = [&](uint32_t (&v)[32], int c, float a, float f) {
+                for (int tries = 0;; ++tries) {
+                    const uint64_t a2 = pair(a, a), c2 = pair(-ref, -ref);
+                    float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int x = 0; x < 64; ++x)
-                        if (x >= first && x < last) most = fmaxf(most, fmaf(__uint_as_float(v[x]), a, -ref));
-                } else {
-#pragma unroll
-                    for (int x = 0; x < 64; ++x) most = fmaxf(most, fmaf(__uint_as_float(v[x]), a, -ref));
-                }
-                if (__any_sync(0xffffffffu, most > kLift + kSlack)) {
+                    for (int x = 0; x < 32; x += 2) {
+                        float y0, y1;
+                        unpair(fma2(pair(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), a2, c2), y0, y1);
+                        v[x] = __float_as_uint(y0);
+                        v[x + 1] = __float_as_uint(y1);
+                        most[x / 2 & 1] = fmaxf(fmaxf(most[x / 2 & 1], y0), y1);
+                    }
+                    if (!__any_sync(0xffffffffu, fmaxf(most[0], most[1]) > kLift + kSlack) || tries == 1) break;
                     // references are whole numbers, so that weights in tensor memory are rescaled without rounding
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int x = 0; x < 64; ++x)
-                        if (x >= first && x < last) top = fmaxf(top, __uint_as_float(v[x]) * a);
-                    top = floorf(top) - kLift;
+                    const float top = floorf(largest_logit(col_s + 32 * c, a)) - kLift;
                     const bool grows = top > ref;
                     const float factor = grows ? fast_exp2(ref - top) : 1.f;
                     l *= factor;
+                    sum[0] = mul2(sum[0], pair(factor, factor));
+                    sum[1] = mul2(sum[1], pair(factor, factor));
                     if (grows) ref = top;
-                    rescale(factor, j > 0, h == 1);
+                    rescale(col_o, j > 0 ? D : 0, col_s, 16 * c, factor);
+                    tmem_ld32(col_s + 32 * c, v);
+                    tmem_wait_ld32(v);
                 }
+                const uint64_t f2 = pair(f, f);
+                uint32_t w[16];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t w[16];
-                    float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float y0 = fmaf(__uint_as_float(v[32 * c + 2 * x]), a, -ref), y1 = fmaf(__uint_as_float(v[32 * c + 2 * x + 1]), a, -ref);
-                        if (masked) {
-                            const int at = 32 * c + 2 * x;
-                            if (at < first || at >= last) y0 = -INFINITY;
-                            if (at + 1 < first || at + 1 >= last) y1 = -INFINITY;
-                        }
-                        const float p0 = fast_exp2(y0), p1 = fast_exp2(y1);
-                        sum0 += p0;
-                        sum1 += p1;
-                        w[x] = pack_f16x2(p0 * f, p1 * f);
-                    }
-                    l += sum0 + sum1;
-                    tmem_st16u(col_s + 32 * h + 16 * c, w);
+                for (int x = 0; x < 16; ++x) {
+                    const uint64_t e = pair(fast_exp2(__uint_as_float(v[2 * x])), fast_exp2(__uint_as_float(v[2 * x + 1])));
+                    sum[x & 1] = add2(sum[x & 1], e);
+                    float lo, hi;
+                    unpair(mul2(e, f2), lo, hi);
+                    w[x] = pack_f16x2(lo, hi);
                 }
+                tmem_st16u(col_s + 16 * c, w);
+            };
+            uint32_t v0[32], v1[32];
+            tmem_ld32(col_s, v0);
+            tmem_wait_ld32(v0);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                tmem_ld32(col_s + 64 * h + 32, v1);          // on their way while the 32 before them are weighed
+                weigh(v0, 2 * h, h ? a[1] : a[0], h ? f[1] : f[0]);
+                tmem_wait_ld32(v1);
+                tmem_ld32(col_s + 64, v0);                   // (once more in the second round, for nobody)
+                weigh(v1, 2 * h + 1, h ? a[1] : a[0], h ? f[1] : f[0]);
+                tmem_wait_ld32(v0);
             }
+            float lo2, hi2;
+            unpair(add2(sum[0], sum[1]), lo2, hi2);
+            l += lo2 + hi2;
             tmem_wait_st();
             tcgen05_fence_before();
             __syncwarp();
@@ -725,7 +833,8 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
         }
         for (int k = 0; k < 4; ++k) {
             mbar_init(bars + 8 * (kBarScale + k), 1);
-            mbar_init(bars + 8 * (kBarSegFull + k), 1); mbar_init(bars + 8 * (kBarSegEmpty + k), 13);
+            mbar_init(bars + 8 * (kBarSegFull + k), 1); mbar_init(bars + 8 * (kBarSegEmpty + k), 9);
+            mbar_init(bars + 8 * (kBarTileFull + k), 1); mbar_init(bars + 8 * (kBarTileEmpty + k), 4);
         }
         misc[1] = 0;
         for (int k = 0; k < kNanBuffers; ++k) reinterpret_cast<int *>(smem + L::kNanAny)[k] = 0;
@@ -744,9 +853,9 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     const Share share = plan(p, worker);
     const Block b = {p, smem, smem_u32(smem), bars, misc[0], Ctx{misc + 1, p.status}};
     if (warp < kWarpConvert) soften<D>(b, warp >> 2, tid & 127, lane);
-    else if (warp < kWarpMma) convert<D>(b, cache, tid - 32 * kWarpConvert, lane);
+    else if (warp < kWarpMma) convert<D>(b, tid - 32 * kWarpConvert, lane);
     else if (warp == kWarpMma) issue<D>(b, lane);
-    else schedule<D>(b, share, worker, lane);
+    else schedule<D>(b, cache, share, worker, lane);
     if (misc[1]) {
         // a wait has given up: MMAs that were issued must be over before the tensor memory is
         const unsigned long long since = global_timer_ns();
