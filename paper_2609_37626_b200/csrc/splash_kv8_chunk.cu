@@ -46,8 +46,8 @@ struct alignas(16) Tile {
 enum { kTileEdge = 1 /* not all rows see all its tokens */, kTileLast = 2 /* of its segment */, kTileEnd = 4 };
 
 enum {                                 // mbarriers
-    kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVEmpty = 6, kBarS = 8, kBarP = 10, kBarQ = 12, kBarO = 14, kBarScale = 16,
-    kBarSegFull = 20, kBarSegEmpty = 24, kBarTileFull = 28, kBarTileEmpty = 32, kNumBars = 36
+    kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVEmpty = 6, kBarS = 8 /* [half][buffer] */, kBarP = 12, kBarQ = 16, kBarO = 18 /* as S */, kBarScale = 22,
+    kBarSegFull = 26, kBarSegEmpty = 30, kBarTileFull = 34, kBarTileEmpty = 38, kNumBars = 42
 };
 
 template <int D>
@@ -64,7 +64,7 @@ struct Layout {
     static constexpr uint32_t kBars = kTiles + 4 * sizeof(Tile);
     static constexpr uint32_t kMisc = kBars + 8 * kNumBars;                // tensor memory address, abort flag
     static constexpr uint32_t kBytes = kMisc + 16 + 1024;
-    static constexpr uint32_t kColS = 0, kColO = 256;                      // tensor memory: S (and P over it) 128 columns a half, O D columns a half
+    static constexpr uint32_t kColS = 0, kColO = 256;                      // tensor memory: two buffers of S (and P over it) of 64 columns a half, O D columns a half
 };
 
 // fp16 operands, fp32 sums
@@ -103,11 +103,13 @@ __device__ __forceinline__ void tmem_wait_ld32(uint32_t (&r)[32]) {
           "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
         :: "memory");
 }
-__device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+          "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
 
 // ---- the cost line --------------------------------------------------------------------------------------------------------
@@ -324,68 +326,73 @@ template <int D>
 __device__ __forceinline__ void issue(const Block &b, int lane) {
     using L = Layout<D>;
     const uint32_t elected = elect_one(), tmem = uniform(b.tmem), base = uniform(b.base);
-    constexpr uint32_t kDescS = idesc_f16(128, 128, 0), kDescO = idesc_f16(128, D, 1);
+    constexpr uint32_t kDescS = idesc_f16(128, kPage, 0), kDescO = idesc_f16(128, D, 1);
     Segments segments{b, L::kSegments};
-    uint32_t it = 0, seg = 0;
+    uint32_t it = 0, pages = 0, seg = 0;              // tiles, pages and segments so far
     bool ok = true;
-    auto logits = [&](int half, uint32_t stage) {
-        const uint64_t q = make_desc(base + L::kQ + half * L::kTile, 16, 1024), k = make_desc(base + L::kK + stage * L::kTile, 16, 1024);
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-            const uint32_t at = ((x >> 2) * L::kSlab + (x & 3) * 32) >> 4;
-            mma_ss(elected, tmem + L::kColS + half * 128, q + at, k + at, kDescS, x != 0);
-        }
-        if (elected) umma_commit(b.bar(kBarS + half));
-        __syncwarp();
-    };
     while (ok) {
         const Segment *const s = segments.take();
         if (s == nullptr) break;
-        const int tiles = (int)uniform((uint32_t)s->tiles);
-        if (tiles > 0) {
-            for (int half = 0; half < 2 && ok; ++half) ok = warp_wait(b.ctx, b.bar(kBarQ + half), seg & 1, kBarQ);
-            if (ok) ok = warp_wait(b.ctx, b.bar(kBarKFull + (it & 1)), (it >> 1) & 1, kBarKFull);
-            if (!ok) break;
+        const int n = s->tiles > 0 ? (int)uniform((uint32_t)((s->hi - s->t0 + kPage - 1) / kPage)) : 0;
+        // S of page u; the stage of its tile is free behind its last page
+        auto logits = [&](int half, int u) {
+            const uint32_t stage = (it + (u >> 1)) & 1, buffer = (pages + u) & 1;
+            const uint64_t q = make_desc(base + L::kQ + half * L::kTile, 16, 1024), k = make_desc(base + L::kK + stage * L::kTile + (u & 1) * kPage * 128, 16, 1024);
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x) {
+                const uint32_t at = ((x >> 2) * L::kSlab + (x & 3) * 32) >> 4;
+                mma_ss(elected, tmem + L::kColS + half * 128 + buffer * 64, q + at, k + at, kDescS, x != 0);
+            }
+            if (elected) {
+                umma_commit(b.bar(kBarS + 2 * half + buffer));
+                if (half == 1 && ((u & 1) || u == n - 1)) umma_commit(b.bar(kBarKEmpty + stage));
+            }
+            __syncwarp();
+        };
+        auto keys_of = [&](int u) {                   // waits for the tile that page u begins
+            if (u & 1) return true;
+            const uint32_t tile = it + (u >> 1);
+            if (!warp_wait(b.ctx, b.bar(kBarKFull + (tile & 1)), (tile >> 1) & 1, kBarKFull)) return false;
             fence_proxy_async();
             tcgen05_fence_after();
-            logits(0, it & 1);
-            logits(1, it & 1);
-            if (elected) umma_commit(b.bar(kBarKEmpty + (it & 1)));
-            __syncwarp();
-            for (int j = 0; ok && j < tiles; ++j, ++it) {
-                const uint32_t stage = it & 1, next = stage ^ 1;
-                ok = warp_wait(b.ctx, b.bar(kBarVFull + stage), (it >> 1) & 1, kBarVFull);
-                fence_proxy_async();
+            return true;
+        };
+        if (n > 0) {
+            for (int half = 0; half < 2 && ok; ++half) ok = warp_wait(b.ctx, b.bar(kBarQ + half), seg & 1, kBarQ);
+            for (int u = 0; ok && u < min(n, 2); ++u) {
+                ok = keys_of(u);
+                if (!ok) break;
+                logits(0, u);
+                logits(1, u);
+            }
+            for (int u = 0; ok && u < n; ++u) {
+                const uint32_t tile = it + (u >> 1), stage = tile & 1, buffer = (pages + u) & 1;
+                if ((u & 1) == 0) {
+                    ok = warp_wait(b.ctx, b.bar(kBarVFull + stage), (tile >> 1) & 1, kBarVFull);
+                    fence_proxy_async();
+                }
                 for (int half = 0; ok && half < 2; ++half) {
-                    ok = warp_wait(b.ctx, b.bar(kBarP + half), it & 1, kBarP);
+                    ok = warp_wait(b.ctx, b.bar(kBarP + 2 * half + buffer), ((pages + u) >> 1) & 1, kBarP);
                     if (!ok) break;
                     tcgen05_fence_after();
-                    const uint64_t v = make_desc(base + L::kV + stage * L::kTile, L::kSlab, 1024);
+                    const uint64_t v = make_desc(base + L::kV + stage * L::kTile + (u & 1) * kPage * 128, L::kSlab, 1024);
 #pragma unroll
-                    for (int x = 0; x < kTileTokens / 16; ++x)
-                        mma_ts(elected, tmem + L::kColO + half * D, tmem + L::kColS + half * 128 + x * 8, v + ((x * 2048) >> 4), kDescO, (uint32_t)j | (uint32_t)x);
-                    if (half == 1) {
-                        if (elected) umma_commit(b.bar(kBarVEmpty + stage));
-                        __syncwarp();
+                    for (int x = 0; x < kPage / 16; ++x)
+                        mma_ts(elected, tmem + L::kColO + half * D, tmem + L::kColS + half * 128 + buffer * 64 + x * 8, v + ((x * 2048) >> 4), kDescO,
+                               (uint32_t)u | (uint32_t)x);
+                    if (elected) {
+                        umma_commit(b.bar(kBarO + 2 * half + buffer));
+                        if (half == 1 && ((u & 1) || u == n - 1)) umma_commit(b.bar(kBarVEmpty + stage));
                     }
-                    if (j + 1 < tiles) {
-                        if (half == 0) {
-                            ok = warp_wait(b.ctx, b.bar(kBarKFull + next), ((it + 1) >> 1) & 1, kBarKFull);
-                            if (!ok) break;
-                            fence_proxy_async();
-                            tcgen05_fence_after();
-                        }
-                        logits(half, next);
-                        if (half == 1) {
-                            if (elected) umma_commit(b.bar(kBarKEmpty + next));
-                            __syncwarp();
-                        }
-                    } else {
-                        if (elected) umma_commit(b.bar(kBarO + half));
-                        __syncwarp();
+                    __syncwarp();
+                    if (u + 2 < n) {
+                        if (half == 0) ok = keys_of(u + 2);
+                        if (ok) logits(half, u + 2);
                     }
                 }
             }
+            it += s->tiles;
+            pages += n;
             ++seg;
         }
         segments.done(lane);
@@ -548,37 +555,24 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
     return r;
 }
 
-// The warp's rows of O (`cols` columns) and of the weights so far (`weights` columns of two fp16 over S), times a factor per row.
-__device__ __noinline__ void rescale(uint32_t col_o, int cols, uint32_t col_p, int weights, float a) {
-    for (int c = 0; c < cols; c += 16) {
+// The warp's rows of O times a factor per row.
+template <int D>
+__device__ __noinline__ void rescale(uint32_t col, float a) {
+    for (int c = 0; c < D; c += 16) {
         float v[16];
-        tmem_ld16(col_o + c, v);
+        tmem_ld16(col + c, v);
         tmem_wait_ld();
 #pragma unroll
         for (int x = 0; x < 16; ++x) v[x] *= a;
-        tmem_st16(col_o + c, v);
+        tmem_st16(col + c, v);
     }
-    const __half2 h = __float2half2_rn(a);
     tmem_wait_st();
-    for (int c = 0; c < weights; c += 16) {
-        float v[16];
-        uint32_t u[16];
-        tmem_ld16(col_p + c, v);
-        tmem_wait_ld();
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            const uint32_t bits = __float_as_uint(v[x]);
-            const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&bits), h);
-            u[x] = *reinterpret_cast<const uint32_t *>(&y);
-        }
-        tmem_st16u(col_p + c, u);
-    }
 }
 
-// The largest of 32 sums, times their factor.
+// The largest of a page's 64 sums, times their factor.
 __device__ __noinline__ float largest_logit(uint32_t col, float a) {
     float top = -INFINITY;
-    for (int c = 0; c < 32; c += 16) {
+    for (int c = 0; c < 64; c += 16) {
         float v[16];
         tmem_ld16(col + c, v);
         tmem_wait_ld();
@@ -626,7 +620,7 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
     const uint32_t lanes = (uint32_t)(r & 96) << 16;
     const uint32_t col_s = b.tmem + lanes + L::kColS + half * 128, col_o = b.tmem + lanes + L::kColO + half * D;
     const float *const scales = reinterpret_cast<const float *>(b.smem + L::kScales);
-    uint32_t it = 0, seg = 0;
+    uint32_t it = 0, pages = 0, seg = 0;
     for (;;) {
         const Segment *const at = segments.take();
         if (at == nullptr) break;
@@ -690,92 +684,77 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
         }
         const int lim = there ? min(s.hi, s.len - s.rows_all + row + 1) : s.hi;
         const int lim_min = __reduce_min_sync(0xffffffffu, lim);
-        const int lo = s.lo, tiles = s.tiles, start = s.t0;
+        const int lo = s.lo, n = (s.hi - s.t0 + kPage - 1) / kPage, start = s.t0;
         float ref = kUnset, l = 0.f, unit = 0.f;
         bool ok = true;
-        for (int j = 0; ok && j < tiles; ++j, ++it) {
-            const int t0 = start + j * kTileTokens;
-            ok = warp_wait(b.ctx, b.bar(kBarScale + (it & 3)), (it >> 2) & 1, kBarScale);
+        for (int u = 0; ok && u < n; ++u) {
+            const uint32_t tile = it + (u >> 1), page = pages + u, buffer = page & 1;
+            const uint32_t col = col_s + buffer * 64;
+            if ((u & 1) == 0) ok = warp_wait(b.ctx, b.bar(kBarScale + (tile & 3)), (tile >> 2) & 1, kBarScale);
             if (!ok) break;
-            const float4 sc = reinterpret_cast<const float4 *>(scales)[it & 3];
-            ok = warp_wait(b.ctx, b.bar(kBarS + half), it & 1, kBarS);
+            float a = back * scales[4 * (tile & 3) + (u & 1)];
+            const float vs = scales[4 * (tile & 3) + 2 + (u & 1)];
+            ok = warp_wait(b.ctx, b.bar(kBarS + 2 * half + buffer), (page >> 1) & 1, kBarS);
             if (!ok) break;
             tcgen05_fence_after();
-            const float largest = fmaxf(fabsf(sc.z), fabsf(sc.w));
-            if (largest > unit) {
-                if (j > 0) rescale(col_o, D, col_s, 0, __fdividef(unit, largest));
-                unit = largest;
-            }
-            float a[2] = {back * sc.x, back * sc.y}, f[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float vsc = h ? sc.w : sc.z;
-                f[h] = vsc == unit ? 1.f : __fdividef(vsc, unit);
-                const int tb = t0 + h * kPage;
-                if (tb < lo || tb + kPage > lim_min) a[h] = hide(col_s + 64 * h, lo - tb, lim - tb, a[h]);
-            }
-            uint64_t sum[2] = {0, 0};
-            // 32 columns: y = x - ref, p = 2^y, to where columns that are done with lie
-            auto weigh = [&](uint32_t (&v)[32], int c, float a, float f) {
-                for (int tries = 0;; ++tries) {
-                    const uint64_t a2 = pair(a, a), c2 = pair(-ref, -ref);
-                    float most[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                    for (int x = 0; x < 32; x += 2) {
-                        float y0, y1;
-                        unpair(fma2(pair(__uint_as_float(v[x]), __uint_as_float(v[x + 1])), a2, c2), y0, y1);
-                        v[x] = __float_as_uint(y0);
-                        v[x + 1] = __float_as_uint(y1);
-                        most[x / 2 & 1] = fmaxf(fmaxf(most[x / 2 & 1], y0), y1);
-                    }
-                    if (!__any_sync(0xffffffffu, fmaxf(most[0], most[1]) > kLift + kSlack) || tries == 1) break;
-                    // references are whole numbers, so that weights in tensor memory are rescaled without rounding
-                    const float top = floorf(largest_logit(col_s + 32 * c, a)) - kLift;
-                    const bool grows = top > ref;
-                    const float factor = grows ? fast_exp2(ref - top) : 1.f;
-                    l *= factor;
-                    sum[0] = mul2(sum[0], pair(factor, factor));
-                    sum[1] = mul2(sum[1], pair(factor, factor));
-                    if (grows) ref = top;
-                    rescale(col_o, j > 0 ? D : 0, col_s, 16 * c, factor);
-                    tmem_ld32(col_s + 32 * c, v);
-                    tmem_wait_ld32(v);
-                }
-                const uint64_t f2 = pair(f, f);
-                uint32_t w[16];
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const uint64_t e = pair(fast_exp2(__uint_as_float(v[2 * x])), fast_exp2(__uint_as_float(v[2 * x + 1])));
-                    sum[x & 1] = add2(sum[x & 1], e);
-                    float lo, hi;
-                    unpair(mul2(e, f2), lo, hi);
-                    w[x] = pack_f16x2(lo, hi);
-                }
-                tmem_st16u(col_s + 16 * c, w);
+            // rescales O, once the MMAs of the page before are done with it
+            auto shrink = [&](float factor) {
+                ok = warp_wait(b.ctx, b.bar(kBarO + 2 * half + (buffer ^ 1)), ((page - 1) >> 1) & 1, kBarO);
+                tcgen05_fence_after();
+                rescale<D>(col_o, factor);
             };
-            uint32_t v0[32], v1[32];
-            tmem_ld32(col_s, v0);
-            tmem_wait_ld32(v0);
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                tmem_ld32(col_s + 64 * h + 32, v1);          // on their way while the 32 before them are weighed
-                weigh(v0, 2 * h, h ? a[1] : a[0], h ? f[1] : f[0]);
-                tmem_wait_ld32(v1);
-                tmem_ld32(col_s + 64, v0);                   // (once more in the second round, for nobody)
-                weigh(v1, 2 * h + 1, h ? a[1] : a[0], h ? f[1] : f[0]);
-                tmem_wait_ld32(v0);
+            if (fabsf(vs) > unit) {
+                if (u > 0) shrink(__fdividef(unit, fabsf(vs)));
+                unit = fabsf(vs);
             }
+            const float f = vs == unit ? 1.f : __fdividef(vs, unit);
+            const int tb = start + u * kPage;
+            if (tb < lo || tb + kPage > lim_min) a = hide(col, lo - tb, lim - tb, a);
+            // y = x - ref, p = 2^y.  Whether a logit exceeds the reference by too much shows while the weights are computed; then they
+            // are computed again (the weights' place is that of the sums: they are written when all of them are known to be right).
+            uint32_t w[32];
+            uint64_t sum[4];
+            for (int tries = 0;; ++tries) {
+                uint32_t v[2][32];
+                tmem_ld32(col, v[0]);
+                tmem_ld32(col + 32, v[1]);
+                tmem_wait_ld32(v[0]);
+                tmem_wait_ld32(v[1]);
+                const uint64_t a2 = pair(a, a), c2 = pair(-ref, -ref), f2 = pair(f, f);
+                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] = 0;
+#pragma unroll
+                for (int x = 0; x < 32; ++x) {
+                    float y0, y1, lo2, hi2;
+                    unpair(fma2(pair(__uint_as_float(v[x >> 4][2 * x & 31]), __uint_as_float(v[x >> 4][(2 * x & 31) + 1])), a2, c2), y0, y1);
+                    most[x & 3] = fmaxf(fmaxf(most[x & 3], y0), y1);
+                    const uint64_t e = pair(fast_exp2(y0), fast_exp2(y1));
+                    sum[x & 3] = add2(sum[x & 3], e);
+                    unpair(mul2(e, f2), lo2, hi2);
+                    w[x] = pack_f16x2(lo2, hi2);
+                }
+                if (!__any_sync(0xffffffffu, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kLift + kSlack) || tries == 1) break;
+                const float top = largest_logit(col, a) - kLift;
+                const bool grows = top > ref;
+                const float factor = grows ? fast_exp2(ref - top) : 1.f;
+                l *= factor;
+                if (grows) ref = top;
+                if (u > 0) shrink(factor);
+            }
+            tmem_st32u(col, w);
             float lo2, hi2;
-            unpair(add2(sum[0], sum[1]), lo2, hi2);
+            unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), lo2, hi2);
             l += lo2 + hi2;
             tmem_wait_st();
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(b.bar(kBarP + half));
+            if (lane == 0) mbar_arrive(b.bar(kBarP + 2 * half + buffer));
         }
         if (!ok) return;
         // ---- epilogue
-        if (!warp_wait(b.ctx, b.bar(kBarO + half), seg & 1, kBarO)) return;
+        const uint32_t end = pages + n - 1;
+        if (!warp_wait(b.ctx, b.bar(kBarO + 2 * half + (end & 1)), (end >> 1) & 1, kBarO)) return;
         tcgen05_fence_after();
         const float scale = l == 0.f ? 0.f : __fdividef(unit, l);
         const float lse2 = l == 0.f ? -INFINITY : ref + __log2f(l);
@@ -810,6 +789,8 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
             else p.part_lse[s.slot * kTileRows + half * 128 + r] = lse2;
         }
         tcgen05_fence_before();
+        it += s.tiles;
+        pages += n;
         segments.done(lane);
         ++seg;
     }
@@ -828,11 +809,11 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
         for (int k = 0; k < 2; ++k) {
             mbar_init(bars + 8 * (kBarKFull + k), 4); mbar_init(bars + 8 * (kBarKEmpty + k), 1);
             mbar_init(bars + 8 * (kBarVFull + k), 4); mbar_init(bars + 8 * (kBarVEmpty + k), 1);
-            mbar_init(bars + 8 * (kBarS + k), 1); mbar_init(bars + 8 * (kBarP + k), 4);
-            mbar_init(bars + 8 * (kBarQ + k), 4); mbar_init(bars + 8 * (kBarO + k), 1);
+            mbar_init(bars + 8 * (kBarQ + k), 4);
         }
         for (int k = 0; k < 4; ++k) {
             mbar_init(bars + 8 * (kBarScale + k), 1);
+            mbar_init(bars + 8 * (kBarS + k), 1); mbar_init(bars + 8 * (kBarP + k), 4); mbar_init(bars + 8 * (kBarO + k), 1);
             mbar_init(bars + 8 * (kBarSegFull + k), 1); mbar_init(bars + 8 * (kBarSegEmpty + k), 9);
             mbar_init(bars + 8 * (kBarTileFull + k), 1); mbar_init(bars + 8 * (kBarTileEmpty + k), 4);
         }
