@@ -105,7 +105,11 @@ struct Plan { int rows, workers, chunk_workers; int64_t pairs; };
 Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
     Plan p;
     p.pairs = (int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads);
-    kv8_decode_shape(p.pairs < kDecodePairs ? p.pairs : kDecodePairs, c->head_dim, sms, &p.rows, &p.workers);
+    const int64_t pairs = p.pairs < kDecodePairs ? p.pairs : kDecodePairs;
+    kv8_decode_shape(pairs, c->head_dim, sms, &p.rows, &p.workers);
+    // no more blocks than the work can cost (an item's overhead is two pages)
+    const int64_t cost = (pairs + p.rows - 1) / p.rows * c->num_kv_heads * s->num_requests * (s->table_width + 2LL);
+    if (cost > 0 && cost < p.workers) p.workers = (int)cost;
     p.chunk_workers = p.pairs > kDecodePairs ? sms : 0;
     return p;
 }

@@ -14,7 +14,7 @@ namespace splash {
 namespace {
 
 constexpr int kSlotThreads = 512;
-constexpr int kPlacesPerThread = 4;
+constexpr int kPlacesPerThread = 1;       // (until there are two blocks for every SM)
 
 struct SlotParams {
     const int32_t *seq_lens, *new_lens, *free_pages, *free_begin;

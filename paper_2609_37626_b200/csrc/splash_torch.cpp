@@ -514,6 +514,14 @@ bool stream_on(PyObject *o, c10::DeviceIndex device, void *&stream) {
     return stream_of(o, stream);
 }
 
+// A 1-D tensor over a part of another one's memory.
+at::Tensor part_of(const at::Tensor &all, int64_t byte, int64_t n, at::ScalarType dtype) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(dtype));
+    t.unsafeGetTensorImpl()->set_storage_offset(byte / (int64_t)t.element_size());
+    t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+    return t;
+}
+
 const char *const kSlotNames[] = {"block_table", "seq_lens", "new_lens", "free_pages", "free_begin", "num_slots", "slot_map", "positions", "q_start",
                                   "new_seq_lens", "counts", "stream"};
 Signature sig_slots{"splash_kv_slots", 6, 6, 12, kSlotNames, nullptr};
@@ -537,9 +545,13 @@ PyObject *kv_slots(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject
     if (!on_one_gpu({table, lens, more, free_pages, begin, given_out[0], given_out[1], given_out[2], given_out[3], given_out[4]})) return nullptr;
     const c10::cuda::CUDAGuard guard(table->device());
     const int64_t sizes[5] = {places, places, B + 1, B, 4};
-    at::Tensor out[5];
+    at::Tensor out[5], all;
+    int64_t bytes = 0, at[5];
+    for (int k = 0; k < 5; ++k)
+        if (given_out[k] == nullptr) { at[k] = bytes; bytes += (sizes[k] * (k == 0 ? 8 : 4) + 255) / 256 * 256; }
+    if (bytes > 0) all = new_tensor({bytes}, at::kByte, *table);      // (one allocation for all: five cost as much as the kernel)
     for (int k = 0; k < 5; ++k) {
-        if (given_out[k] == nullptr) { out[k] = new_tensor({sizes[k]}, k == 0 ? at::kLong : at::kInt, *table); continue; }
+        if (given_out[k] == nullptr) { out[k] = part_of(all, at[k], sizes[k], k == 0 ? at::kLong : at::kInt); continue; }
         out[k] = *given_out[k];
         SPLASH_ASSERT(out[k].dim() == 1 && out[k].numel() == sizes[k] && out[k].is_contiguous() && out[k].scalar_type() == (k == 0 ? at::kLong : at::kInt));
     }
