@@ -16,6 +16,7 @@ cudaError_t launch_kv8_append(const splash_kv8_cache &cache, int32_t dtype, int6
 void kv8_decode_shape(int64_t pairs, int head_dim, int sm_count, int *rows, int *workers);
 bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v_map);
 int kv8_chunk_rows();
+int kv8_chunk_workers(int sm_count);
 cudaError_t launch_kv8_chunk(const kv8::AttnParams &p, const splash_kv8_cache &cache, cudaStream_t stream);
 cudaError_t launch_kv8_decode(const kv8::AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream);
 
@@ -107,10 +108,10 @@ Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
     p.pairs = (int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads);
     const int64_t pairs = p.pairs < kDecodePairs ? p.pairs : kDecodePairs;
     kv8_decode_shape(pairs, c->head_dim, sms, &p.rows, &p.workers);
-    // no more blocks than the work can cost (an item's overhead is two pages)
-    const int64_t cost = (pairs + p.rows - 1) / p.rows * c->num_kv_heads * s->num_requests * (s->table_width + 2LL);
+    // no more blocks than the work can cost (with its overhead of five pages)
+    const int64_t cost = (pairs + p.rows - 1) / p.rows * c->num_kv_heads * s->num_requests * (s->table_width + 5LL);
     if (cost > 0 && cost < p.workers) p.workers = (int)cost;
-    p.chunk_workers = p.pairs > kDecodePairs ? sms : 0;
+    p.chunk_workers = p.pairs > kDecodePairs ? kv8_chunk_workers(sms) : 0;
     return p;
 }
 

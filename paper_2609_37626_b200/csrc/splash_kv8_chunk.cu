@@ -1,16 +1,18 @@
-// Attention of many query rows (chunks of prompts) over a paged cache of keys and values in e4m3 with a scale per (page, head).
+// Attention of more than a few query rows (chunks of prompts, drafted rows) over a paged cache of keys and values in e4m3 with a scale per
+// (page, head).
 //
-// The (row, head) pairs of a request and key head, m = row * group + head, are cut in tiles of 256; an item of work is (request, key head, tile).
-// Tokens come 128 at a time (two pages).  Tensor cores bound it: per 128 tokens 2 x 16 MMAs of 128 x 128 x 16 take 2,048 cycles, and the
-// 32,768 exponentials as long.  One block an SM, 14 warps:
-//   - 4 converter warps read codes (16 bytes a lane), widen them to fp16 (exact) and lay them out in shared memory, keys K-major and values MN-major in
-//     the 128-byte swizzle, two stages each.  They pay for 256 query rows at once: per code half a conversion and two bytes of stores.
-//   - 1 warp issues tcgen05.mma: S = Q K^T from shared memory into tensor memory; O += P V with P read from tensor memory, where the softmax
-//     leaves it over S.  The halves of the tile (128 rows each) take turns: while one's softmax runs, the tensor cores work for the other.
-//   - 2 x 4 softmax warps, a thread per row: p = 2^(x - m + 7) with a reference m that moves only when a logit exceeds it by 8 (then O, the sum, and what
-//     has been written of P are rescaled), p rounded to fp16, value scales folded into p as v_scale / U with U the largest so far.
-//   - 1 scheduler warp walks the worker's share of the cost line and publishes segments (an item's range of tokens) ahead of the others.
-// The line counts token tiles up to the tile's last causal row, and kOverhead per item (queries, epilogue); items cut by a share's end are joined by the
+// The (row, head) pairs of a request and key head, m = row * group + head, are cut in tiles of 128; an item of work is (request, key head, tile).
+// Two blocks of 10 warps share an SM, each with its own item, so that one's queries and outputs pass while the other works:
+//   - 4 converter warps read a page's codes (16 bytes a lane), widen them to fp16 (exact) and lay them out in shared memory, keys K-major and values
+//     MN-major in the 128-byte swizzle, two stages each;
+//   - 1 warp issues tcgen05.mma: S = Q K^T from shared memory into one of two buffers in tensor memory; O += P V with P read from tensor memory, where the
+//     softmax leaves it over S.  While the softmax has page u, S of page u + 1 is there and O of page u - 1 under way;
+//   - 4 softmax warps, a thread per row: p = 2^(x - m + 7) with a reference m that moves only when a logit exceeds it by 8 (then O and the sum are
+//     rescaled), p rounded to fp16, value scales folded into p as v_scale / U with U the largest so far;
+//   - 1 scheduler warp walks the worker's share of the cost line and publishes segments (an item's range of pages) and their pages ahead of the others.
+// Shared memory bounds it: a page costs 32 KB of stores, 16 KB for K and for V and 32 KB for Q, 768 cycles at 128 bytes, against 640 of MMAs and 512 of
+// exponentials.
+// The line counts pages up to the tile's last causal row, and kOverhead per item (queries, epilogue); items cut by a share's end are joined by the
 // combine kernel of the decode path.
 #include "splash_kv8.cuh"
 #include "splash_umma.cuh"
@@ -22,10 +24,10 @@ namespace {
 using namespace kv8;
 using namespace umma;
 
-constexpr int kTileRows = 256, kTileTokens = 128;
-constexpr int kOverhead = 3;                       // cost of an item beside its tiles, in tiles of 128 tokens
-constexpr int kMinUnits = 4;                       // least cost of a worker's share
-constexpr int kWarpConvert = 8, kWarpMma = 12, kThreads = 32 * 14;      // (softmax 0 to 7, scheduler 13)
+constexpr int kTileRows = 128;
+constexpr int kOverhead = 6;                       // cost of an item beside its pages, in pages
+constexpr int kMinUnits = 8;                       // least cost of a worker's share
+constexpr int kWarpConvert = 4, kWarpMma = 8, kThreads = 32 * 10;      // (softmax 0 to 3, scheduler 9)
 constexpr int kNanBuffers = 8;
 
 enum { kEmptyItem = 1, kEndOfWork = 2 };
@@ -33,38 +35,37 @@ enum { kEmptyItem = 1, kEndOfWork = 2 };
 struct alignas(16) Segment {
     int request, row0, rows_all, pairs;
     int m0, head, len, lo;             // lo, hi: tokens of the segment that the tile's last row sees
-    int hi, t0, tiles, slot;           // t0: first token of the first tile (a page's first)
+    int hi, t0, pages, slot;           // t0: first token of the first page
     int flags, pad[3];
 };
 
-// A tile of 128 tokens for the converters: its two pages' rows of the key head (NULL: none, zeros) and their scales.
-struct alignas(16) Tile {
-    const uint8_t *keys[2], *values[2];
-    float k_scale[2], v_scale[2];
+// A page for the converters: the rows of the key head (NULL: no page of the pool, zeros) and their scales.
+struct alignas(16) Page {
+    const uint8_t *keys, *values;
+    float k_scale, v_scale;
     int t0, lo, hi, flags;
 };
-enum { kTileEdge = 1 /* not all rows see all its tokens */, kTileLast = 2 /* of its segment */, kTileEnd = 4 };
+enum { kPageEdge = 1 /* not all rows see all its tokens */, kPageLast = 2 /* of its segment */, kPageEnd = 4 };
 
 enum {                                 // mbarriers
-    kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVEmpty = 6, kBarS = 8 /* [half][buffer] */, kBarP = 12, kBarQ = 16, kBarO = 18 /* as S */, kBarScale = 22,
-    kBarSegFull = 26, kBarSegEmpty = 30, kBarTileFull = 34, kBarTileEmpty = 38, kNumBars = 42
+    kBarKFull = 0, kBarKEmpty = 2, kBarVFull = 4, kBarVEmpty = 6, kBarS = 8 /* [buffer] */, kBarP = 10, kBarO = 12, kBarQ = 14, kBarScale = 15,
+    kBarSegFull = 19, kBarSegEmpty = 23, kBarPageFull = 27, kBarPageEmpty = 31, kNumBars = 35
 };
 
 template <int D>
 struct Layout {
-    static constexpr uint32_t kSlab = 128 * 128;                           // 128 rows of 64 fp16 values
-    static constexpr uint32_t kTile = kSlab * (D / 64);                    // 128 rows of D
-    static constexpr uint32_t kQ = 0;                                      // two halves of the row tile
-    static constexpr uint32_t kK = kQ + 2 * kTile, kV = kK + 2 * kTile;    // two stages each
-    static constexpr uint32_t kNan = kV + 2 * kTile;                       // [8][D] first token with a NaN in dimension d, per segment
+    static constexpr uint32_t kSlabs = D / 64;                             // of 64 fp16 values a row
+    static constexpr uint32_t kQSlab = kTileRows * 128, kSlab = kPage * 128, kTile = kSlab * kSlabs;
+    static constexpr uint32_t kQ = 0, kK = kQ + kQSlab * kSlabs, kV = kK + 2 * kTile;      // K and V: two stages each
+    static constexpr uint32_t kNan = kV + 2 * kTile;                       // [8][128] first token with a NaN in dimension d, per segment
     static constexpr uint32_t kNanAny = kNan + kNanBuffers * 128 * 4;      // [8]
-    static constexpr uint32_t kScales = kNanAny + 32;                      // [4] tiles: two key scales, two value scales
-    static constexpr uint32_t kSegments = kScales + 64;                    // [4]
-    static constexpr uint32_t kTiles = kSegments + 4 * sizeof(Segment);    // [4]
-    static constexpr uint32_t kBars = kTiles + 4 * sizeof(Tile);
-    static constexpr uint32_t kMisc = kBars + 8 * kNumBars;                // tensor memory address, abort flag
+    static constexpr uint32_t kScales = kNanAny + 32;                      // [4] pages: key scale, value scale
+    static constexpr uint32_t kSegments = kScales + 32;                    // [4]
+    static constexpr uint32_t kPages = kSegments + 4 * sizeof(Segment);    // [4]
+    static constexpr uint32_t kBars = kPages + 4 * sizeof(Page);
+    static constexpr uint32_t kMisc = kBars + 8 * kNumBars + 8;            // tensor memory address, abort flag
     static constexpr uint32_t kBytes = kMisc + 16 + 1024;
-    static constexpr uint32_t kColS = 0, kColO = 256;                      // tensor memory: two buffers of S (and P over it) of 64 columns a half, O D columns a half
+    static constexpr uint32_t kColS = 0, kColO = 128, kColumns = 256;      // tensor memory: two buffers of S (and P over it) of 64 columns, O in D columns
 };
 
 // fp16 operands, fp32 sums
@@ -114,13 +115,13 @@ __device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t (&r)[3
 
 // ---- the cost line --------------------------------------------------------------------------------------------------------
 
-// Tokens that tile t of a request sees, and how many tiles of 128 from its first page on: its last row's range.
-struct TileRange { int hi, tiles; };
+// Tokens that row tile t of a request sees, and the pages that they lie in: its last row's range.
+struct TileRange { int hi, pages; };
 __device__ __forceinline__ TileRange tile_range(const AttnParams &p, const Request &r, int t) {
     const int last = (min((t + 1) * kTileRows, r.pairs) - 1) / p.group;
     TileRange x;
     x.hi = min(r.hi, r.len - r.rows_all + last + 1);
-    x.tiles = x.hi > r.lo ? (x.hi - r.lo / kPage * kPage + kTileTokens - 1) / kTileTokens : 0;
+    x.pages = x.hi > r.lo ? (x.hi + kPage - 1) / kPage - r.lo / kPage : 0;
     return x;
 }
 __device__ __forceinline__ int row_tiles(const AttnParams &p, const Request &r) {
@@ -130,7 +131,7 @@ __device__ __forceinline__ int row_tiles(const AttnParams &p, const Request &r) 
 __device__ __forceinline__ int64_t head_units(const AttnParams &p, const Request &r) {
     int64_t n = 0;
     const int tiles = row_tiles(p, r);
-    for (int t = 0; t < tiles; ++t) n += kOverhead + tile_range(p, r, t).tiles;
+    for (int t = 0; t < tiles; ++t) n += kOverhead + tile_range(p, r, t).pages;
     return n;
 }
 
@@ -159,7 +160,7 @@ __device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
         if (w < warp) before += sums[w];
         s.total += sums[w];
     }
-    // (every worker's share is worth a tile at least, so that each from an item's first to its last has a piece of it)
+    // (every worker's share is worth a page at least, so that each from an item's first to its last has a piece of it)
     s.workers = (int)max((int64_t)1, min((int64_t)p.workers, s.total / kMinUnits));
     s.begin = worker < s.workers ? s.total * worker / s.workers : s.total;
     s.end = worker < s.workers ? s.total * (worker + 1) / s.workers : s.total;
@@ -209,8 +210,8 @@ struct Segments {
 template <int D>
 __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache &cache, const Share &share, int worker, int lane) {
     const AttnParams &p = b.p;
-    Tile *const tiles_ring = reinterpret_cast<Tile *>(b.smem + Layout<D>::kTiles);
-    uint32_t tile_at = 0;
+    Page *const pages_ring = reinterpret_cast<Page *>(b.smem + Layout<D>::kPages);
+    uint32_t page_at = 0;
     Segment *const ring = reinterpret_cast<Segment *>(b.smem + Layout<D>::kSegments);
     uint32_t at = 0;
     bool ok = true, has_cut = false;
@@ -224,35 +225,32 @@ __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache 
         __syncwarp();
         ++at;
     };
-    // the segment's tiles: a lane each finds its pages and scales
-    auto publish_tiles = [&](const Segment &s) {
-        for (int j0 = 0; ok && j0 < s.tiles; j0 += 32) {
+    // the segment's pages: a lane each finds one and its scales
+    auto publish_pages = [&](const Segment &s) {
+        for (int j0 = 0; ok && j0 < s.pages; j0 += 32) {
             const int j = j0 + lane;
-            Tile t = {};
-            t.t0 = s.t0 + j * kTileTokens; t.lo = s.lo; t.hi = s.hi;
-            if (j < s.tiles) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = t.t0 + k * kPage, id = at < s.hi ? load_l2(p.table + s.request * p.table_stride + at / kPage) : -1;
-                    if (id >= 0 && id < p.num_pages) {
-                        t.keys[k] = static_cast<const uint8_t *>(cache.k_pool) + id * cache.k_page_stride + s.head * cache.k_head_stride;
-                        t.values[k] = static_cast<const uint8_t *>(cache.v_pool) + id * cache.v_page_stride + s.head * cache.v_head_stride;
-                        t.k_scale[k] = p.k_scales[id * p.k_scale_stride + s.head];
-                        t.v_scale[k] = p.v_scales[id * p.v_scale_stride + s.head];
-                    }
+            Page t = {};
+            t.t0 = s.t0 + j * kPage; t.lo = s.lo; t.hi = s.hi;
+            if (j < s.pages) {
+                const int id = load_l2(p.table + s.request * p.table_stride + t.t0 / kPage);
+                if (id >= 0 && id < p.num_pages) {
+                    t.keys = static_cast<const uint8_t *>(cache.k_pool) + id * cache.k_page_stride + s.head * cache.k_head_stride;
+                    t.values = static_cast<const uint8_t *>(cache.v_pool) + id * cache.v_page_stride + s.head * cache.v_head_stride;
+                    t.k_scale = p.k_scales[id * p.k_scale_stride + s.head];
+                    t.v_scale = p.v_scales[id * p.v_scale_stride + s.head];
                 }
-                if (t.t0 < s.lo || t.t0 + kTileTokens > min(s.hi, s.len - s.rows_all + s.m0 / p.group + 1)) t.flags |= kTileEdge;
-                if (j + 1 == s.tiles) t.flags |= kTileLast;
+                if (t.t0 < s.lo || t.t0 + kPage > min(s.hi, s.len - s.rows_all + s.m0 / p.group + 1)) t.flags |= kPageEdge;
+                if (j + 1 == s.pages) t.flags |= kPageLast;
             }
-            for (int k = 0; ok && k < 32 && j0 + k < s.tiles; ++k) {
-                ok = warp_wait(b.ctx, b.bar(kBarTileEmpty + (tile_at & 3)), ((tile_at >> 2) & 1) ^ 1, kBarTileEmpty);
+            for (int k = 0; ok && k < 32 && j0 + k < s.pages; ++k) {
+                ok = warp_wait(b.ctx, b.bar(kBarPageEmpty + (page_at & 3)), ((page_at >> 2) & 1) ^ 1, kBarPageEmpty);
                 if (!ok) break;
                 if (lane == k) {
-                    tiles_ring[tile_at & 3] = t;
-                    mbar_arrive(b.bar(kBarTileFull + (tile_at & 3)));
+                    pages_ring[page_at & 3] = t;
+                    mbar_arrive(b.bar(kBarPageFull + (page_at & 3)));
                 }
                 __syncwarp();
-                ++tile_at;
+                ++page_at;
             }
         }
     };
@@ -264,7 +262,7 @@ __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache 
         head = (int)(share.u0 / per_head);
         int64_t u = share.u0 - head * per_head;
         for (;; ++t) {
-            const int cost = kOverhead + tile_range(p, r, t).tiles;
+            const int cost = kOverhead + tile_range(p, r, t).pages;
             if (u < cost) break;
             u -= cost;
         }
@@ -276,18 +274,17 @@ __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache 
         for (; ok && head < p.kv_heads && line < share.end; ++head, t = 0)
             for (; ok && t < tiles && line < share.end; ++t) {
                 const TileRange x = tile_range(p, r, t);
-                const int64_t first = line + kOverhead, end = first + x.tiles;
+                const int64_t first = line + kOverhead, end = first + x.pages;
                 const bool mine = line >= share.begin;           // where items are not cut: the worker's that holds its first unit
                 const int64_t from = p.whole ? (mine ? first : end) : max(first, share.begin), to = p.whole ? end : min(end, share.end);
                 Segment s = {};
                 s.request = i; s.row0 = r.row0; s.rows_all = r.rows_all; s.pairs = r.pairs; s.m0 = t * kTileRows; s.head = head; s.len = r.len;
                 s.slot = -1;
                 if (from < to) {
-                    const int start = r.lo / kPage * kPage;
-                    s.tiles = (int)(to - from);
-                    s.t0 = start + (int)(from - first) * kTileTokens;
+                    s.pages = (int)(to - from);
+                    s.t0 = (r.lo / kPage + (int)(from - first)) * kPage;
                     s.lo = max(r.lo, s.t0);
-                    s.hi = to == end ? x.hi : s.t0 + s.tiles * kTileTokens;
+                    s.hi = to == end ? x.hi : s.t0 + s.pages * kPage;
                     s.slot = from > first ? 2 * worker : to < end ? 2 * worker + 1 : -1;
                     if (from == first && to < end) {
                         if (lane == 0) {
@@ -298,8 +295,8 @@ __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache 
                         has_cut = true;
                     }
                     publish(s);
-                    publish_tiles(s);
-                } else if (x.tiles == 0 && mine) {
+                    publish_pages(s);
+                } else if (x.pages == 0 && mine) {
                     s.flags = kEmptyItem;
                     publish(s);
                 }
@@ -311,10 +308,10 @@ __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache 
         Segment s = {};
         s.flags = kEndOfWork;
         publish(s);
-        if (ok) ok = warp_wait(b.ctx, b.bar(kBarTileEmpty + (tile_at & 3)), ((tile_at >> 2) & 1) ^ 1, kBarTileEmpty);
+        if (ok) ok = warp_wait(b.ctx, b.bar(kBarPageEmpty + (page_at & 3)), ((page_at >> 2) & 1) ^ 1, kBarPageEmpty);
         if (ok && lane == 0) {
-            tiles_ring[tile_at & 3].flags = kTileEnd;
-            mbar_arrive(b.bar(kBarTileFull + (tile_at & 3)));
+            pages_ring[page_at & 3].flags = kPageEnd;
+            mbar_arrive(b.bar(kBarPageFull + (page_at & 3)));
         }
     }
     if (!has_cut && !p.whole && lane == 0) p.cut[2 * worker] = make_int4(0, 0, 0, 0);
@@ -326,72 +323,52 @@ template <int D>
 __device__ __forceinline__ void issue(const Block &b, int lane) {
     using L = Layout<D>;
     const uint32_t elected = elect_one(), tmem = uniform(b.tmem), base = uniform(b.base);
-    constexpr uint32_t kDescS = idesc_f16(128, kPage, 0), kDescO = idesc_f16(128, D, 1);
+    constexpr uint32_t kDescS = idesc_f16(kTileRows, kPage, 0), kDescO = idesc_f16(kTileRows, D, 1);
     Segments segments{b, L::kSegments};
-    uint32_t it = 0, pages = 0, seg = 0;              // tiles, pages and segments so far
+    uint32_t pages = 0, seg = 0;                      // pages and segments so far
     bool ok = true;
+    // S of a page, when its keys are there
+    auto logits = [&](uint32_t page) {
+        const uint32_t stage = page & 1;
+        if (!warp_wait(b.ctx, b.bar(kBarKFull + stage), (page >> 1) & 1, kBarKFull)) return false;
+        fence_proxy_async();
+        tcgen05_fence_after();
+        const uint64_t q = make_desc(base + L::kQ, 16, 1024), k = make_desc(base + L::kK + stage * L::kTile, 16, 1024);
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x)
+            mma_ss(elected, tmem + L::kColS + stage * 64, q + (((x >> 2) * L::kQSlab + (x & 3) * 32) >> 4), k + (((x >> 2) * L::kSlab + (x & 3) * 32) >> 4), kDescS, x != 0);
+        if (elected) {
+            umma_commit(b.bar(kBarS + stage));
+            umma_commit(b.bar(kBarKEmpty + stage));
+        }
+        __syncwarp();
+        return true;
+    };
     while (ok) {
         const Segment *const s = segments.take();
         if (s == nullptr) break;
-        const int n = s->tiles > 0 ? (int)uniform((uint32_t)((s->hi - s->t0 + kPage - 1) / kPage)) : 0;
-        // S of page u; the stage of its tile is free behind its last page
-        auto logits = [&](int half, int u) {
-            const uint32_t stage = (it + (u >> 1)) & 1, buffer = (pages + u) & 1;
-            const uint64_t q = make_desc(base + L::kQ + half * L::kTile, 16, 1024), k = make_desc(base + L::kK + stage * L::kTile + (u & 1) * kPage * 128, 16, 1024);
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x) {
-                const uint32_t at = ((x >> 2) * L::kSlab + (x & 3) * 32) >> 4;
-                mma_ss(elected, tmem + L::kColS + half * 128 + buffer * 64, q + at, k + at, kDescS, x != 0);
-            }
-            if (elected) {
-                umma_commit(b.bar(kBarS + 2 * half + buffer));
-                if (half == 1 && ((u & 1) || u == n - 1)) umma_commit(b.bar(kBarKEmpty + stage));
-            }
-            __syncwarp();
-        };
-        auto keys_of = [&](int u) {                   // waits for the tile that page u begins
-            if (u & 1) return true;
-            const uint32_t tile = it + (u >> 1);
-            if (!warp_wait(b.ctx, b.bar(kBarKFull + (tile & 1)), (tile >> 1) & 1, kBarKFull)) return false;
-            fence_proxy_async();
-            tcgen05_fence_after();
-            return true;
-        };
+        const int n = (int)uniform((uint32_t)s->pages);
         if (n > 0) {
-            for (int half = 0; half < 2 && ok; ++half) ok = warp_wait(b.ctx, b.bar(kBarQ + half), seg & 1, kBarQ);
-            for (int u = 0; ok && u < min(n, 2); ++u) {
-                ok = keys_of(u);
-                if (!ok) break;
-                logits(0, u);
-                logits(1, u);
-            }
+            ok = warp_wait(b.ctx, b.bar(kBarQ), seg & 1, kBarQ);
+            for (int u = 0; ok && u < min(n, 2); ++u) ok = logits(pages + u);
             for (int u = 0; ok && u < n; ++u) {
-                const uint32_t tile = it + (u >> 1), stage = tile & 1, buffer = (pages + u) & 1;
-                if ((u & 1) == 0) {
-                    ok = warp_wait(b.ctx, b.bar(kBarVFull + stage), (tile >> 1) & 1, kBarVFull);
-                    fence_proxy_async();
-                }
-                for (int half = 0; ok && half < 2; ++half) {
-                    ok = warp_wait(b.ctx, b.bar(kBarP + 2 * half + buffer), ((pages + u) >> 1) & 1, kBarP);
-                    if (!ok) break;
-                    tcgen05_fence_after();
-                    const uint64_t v = make_desc(base + L::kV + stage * L::kTile + (u & 1) * kPage * 128, L::kSlab, 1024);
+                const uint32_t page = pages + u, stage = page & 1;
+                ok = warp_wait(b.ctx, b.bar(kBarVFull + stage), (page >> 1) & 1, kBarVFull);
+                if (ok) ok = warp_wait(b.ctx, b.bar(kBarP + stage), (page >> 1) & 1, kBarP);
+                if (!ok) break;
+                fence_proxy_async();
+                tcgen05_fence_after();
+                const uint64_t v = make_desc(base + L::kV + stage * L::kTile, L::kSlab, 1024);
 #pragma unroll
-                    for (int x = 0; x < kPage / 16; ++x)
-                        mma_ts(elected, tmem + L::kColO + half * D, tmem + L::kColS + half * 128 + buffer * 64 + x * 8, v + ((x * 2048) >> 4), kDescO,
-                               (uint32_t)u | (uint32_t)x);
-                    if (elected) {
-                        umma_commit(b.bar(kBarO + 2 * half + buffer));
-                        if (half == 1 && ((u & 1) || u == n - 1)) umma_commit(b.bar(kBarVEmpty + stage));
-                    }
-                    __syncwarp();
-                    if (u + 2 < n) {
-                        if (half == 0) ok = keys_of(u + 2);
-                        if (ok) logits(half, u + 2);
-                    }
+                for (int x = 0; x < kPage / 16; ++x)
+                    mma_ts(elected, tmem + L::kColO, tmem + L::kColS + stage * 64 + x * 8, v + ((x * 2048) >> 4), kDescO, (uint32_t)u | (uint32_t)x);
+                if (elected) {
+                    umma_commit(b.bar(kBarO + stage));
+                    umma_commit(b.bar(kBarVEmpty + stage));
                 }
+                __syncwarp();
+                if (u + 2 < n) ok = logits(page + 2);
             }
-            it += s->tiles;
             pages += n;
             ++seg;
         }
@@ -399,41 +376,34 @@ __device__ __forceinline__ void issue(const Block &b, int lane) {
     }
 }
 
-// Codes of one tile's keys or values in registers on their way.  A lane has 16 bytes of rows 32 k + row in each slab of 64 dimensions, row = 8 warp +
-// lane / 4: row mod 8, and with it the swizzle, is the same for all of them, and eight lanes' stores (four chunks of an even and of an odd
+// Codes of one page's keys or values in registers on their way.  A lane has 16 bytes of rows `row` and row + 32 in each slab of 64 dimensions, row =
+// 8 warp + lane / 4: row mod 8, and with it the swizzle, is the same for all of them, and eight lanes' stores (four chunks of an even and of an odd
 // row) meet no bank twice.
 template <int D>
 struct Codes {
-    static constexpr int kSlabs = D / 64, kUnits = 4 * kSlabs;
+    static constexpr int kSlabs = D / 64, kUnits = 2 * kSlabs;
     uint4 w[kUnits];
     static __device__ __forceinline__ int row_of(int tid) { return (tid >> 5) * 8 + (tid >> 2 & 7); }
-    // page k: the pages of the tile's first and last 64 tokens, NULL: zeros; edge: tokens outside [lo, hi) are zeros too
-    __device__ __forceinline__ void load(const uint8_t *page0, const uint8_t *page1, bool edge, int t0, int lo, int hi, int tid) {
+    // page NULL: zeros; edge: tokens outside [lo, hi) are zeros too
+    __device__ __forceinline__ void load(const uint8_t *page, bool edge, int t0, int lo, int hi, int tid) {
         const int row = row_of(tid), at = row * D + (tid & 3) * 16;
-        if (!edge && page0 != nullptr && page1 != nullptr) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int x = 0; x < kSlabs; ++x) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>((k < 2 ? page0 : page1) + at + (k & 1) * 32 * D + x * 64);
-            return;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint8_t *const page = k < 2 ? page0 : page1;
+        for (int k = 0; k < 2; ++k) {
             const int t = t0 + 32 * k + row;
+            const bool there = page != nullptr && (!edge || (t >= lo && t < hi));
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) {
                 w[k * kSlabs + x] = make_uint4(0, 0, 0, 0);
-                if (page != nullptr && t >= lo && t < hi) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>(page + at + (k & 1) * 32 * D + x * 64);
+                if (there) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>(page + at + k * 32 * D + x * 64);
             }
         }
     }
-    // as fp16 into a stage: rows of 64 values in the 128-byte swizzle, slabs of 128 rows
+    // as fp16 into a stage: rows of 64 values in the 128-byte swizzle, slabs of 64 rows
     __device__ __forceinline__ void store(uint8_t *stage, int tid) const {
         const int row = row_of(tid), unit = 2 * (tid & 3);
         uint8_t *const even = stage + row * 128 + ((unit ^ (row & 7)) << 4), *const odd = stage + row * 128 + (((unit + 1) ^ (row & 7)) << 4);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) {
                 const uint4 c = w[k * kSlabs + x];
@@ -456,7 +426,7 @@ struct Codes {
         if ((found & 0x80808080u) == 0) return;
         *any = 1;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) {
                 const uint4 c = w[k * kSlabs + x];
@@ -478,56 +448,53 @@ __device__ __forceinline__ void convert(const Block &b, int tid, int lane) {
     using L = Layout<D>;
     int *const nan = reinterpret_cast<int *>(b.smem + L::kNan), *const nan_any = reinterpret_cast<int *>(b.smem + L::kNanAny);
     float *const scales = reinterpret_cast<float *>(b.smem + L::kScales);
-    const Tile *const ring = reinterpret_cast<const Tile *>(b.smem + L::kTiles);
-    // codes are fetched a tile ahead, keys behind the conversion of keys and values behind that of values
+    const Page *const ring = reinterpret_cast<const Page *>(b.smem + L::kPages);
+    // codes are fetched a page ahead, keys behind the conversion of keys and values behind that of values
     Codes<D> keys, values;
-    uint32_t it = 0, seg = 0;
+    uint32_t page = 0, seg = 0;
     bool begins = true;
-    if (!warp_wait(b.ctx, b.bar(kBarTileFull), 0, kBarTileFull)) return;
-    bool there = !(ring[0].flags & kTileEnd);
-    auto fetch_keys = [&](const Tile &t) { keys.load(t.keys[0], t.keys[1], t.flags & kTileEdge, t.t0, t.lo, t.hi, tid); };
-    auto fetch_values = [&](const Tile &t) { values.load(t.values[0], t.values[1], t.flags & kTileEdge, t.t0, t.lo, t.hi, tid); };
+    if (!warp_wait(b.ctx, b.bar(kBarPageFull), 0, kBarPageFull)) return;
+    bool there = !(ring[0].flags & kPageEnd);
+    auto fetch_keys = [&](const Page &t) { keys.load(t.keys, t.flags & kPageEdge, t.t0, t.lo, t.hi, tid); };
+    auto fetch_values = [&](const Page &t) { values.load(t.values, t.flags & kPageEdge, t.t0, t.lo, t.hi, tid); };
     if (there) { fetch_keys(ring[0]); fetch_values(ring[0]); }
     while (there) {
-        const uint32_t stage = it & 1, turn = it & 3;
-        const Tile &now = ring[turn], &next = ring[(it + 1) & 3];
+        const uint32_t stage = page & 1, turn = page & 3, phase = (page >> 1) & 1;
+        const Page &now = ring[turn], &next = ring[(page + 1) & 3];
         const int flags = now.flags;
         int *const first = nan + (seg & (kNanBuffers - 1)) * 128, *const any = nan_any + (seg & (kNanBuffers - 1));
-        if (begins) {         // a warp is at most two tiles ahead of another, and the softmax warps at most two segments behind
+        if (begins) {         // a warp is at most two pages ahead of another, and the softmax warps at most two segments behind
             nan[((seg + 2) & (kNanBuffers - 1)) * 128 + tid] = 0x7fffffff;
             if (tid == 0) nan_any[(seg + 2) & (kNanBuffers - 1)] = 0;
         }
-        if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), ((it >> 1) & 1) ^ 1, kBarKEmpty)) return;
+        if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), phase ^ 1, kBarKEmpty)) return;
         keys.store(b.smem + L::kK + stage * L::kTile, tid);
-        if (flags & kTileEdge) {
-            for (int k = 0; k < 2; ++k)
-                if (!isfinite(now.v_scale[k])) {         // every value of the page is NaN, for the rows that see a token of it
-                    if (tid < D) atomicMin(first + tid, max(now.lo, now.t0 + k * kPage));
-                    *any = 1;
-                }
+        const float vs = now.v_scale;
+        if ((flags & kPageEdge) && !isfinite(vs)) {      // every value of the page is NaN, for the rows that see a token of it
+            if (tid < D) atomicMin(first + tid, max(now.lo, now.t0));
+            *any = 1;
         }
-        if (tid < 4) {
-            float x = tid < 2 ? now.k_scale[tid] : now.v_scale[tid - 2];
-            if (tid >= 2 && !isfinite(x)) x = flags & kTileEdge ? 0.f : NAN;
-            scales[4 * turn + tid] = x;
+        if (tid == 0) {
+            scales[2 * turn] = now.k_scale;
+            scales[2 * turn + 1] = isfinite(vs) ? vs : flags & kPageEdge ? 0.f : NAN;
+            mbar_arrive(b.bar(kBarScale + turn));
         }
         __syncwarp();
-        if (tid == 0) mbar_arrive(b.bar(kBarScale + turn));
         if (lane == 0) mbar_arrive(b.bar(kBarKFull + stage));
-        if (!warp_wait(b.ctx, b.bar(kBarTileFull + ((it + 1) & 3)), ((it + 1) >> 2) & 1, kBarTileFull)) return;
-        there = !(next.flags & kTileEnd);
+        if (!warp_wait(b.ctx, b.bar(kBarPageFull + ((page + 1) & 3)), ((page + 1) >> 2) & 1, kBarPageFull)) return;
+        there = !(next.flags & kPageEnd);
         if (there) fetch_keys(next);
-        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), ((it >> 1) & 1) ^ 1, kBarVEmpty)) return;
-        if (flags & kTileEdge) values.take_out_nan(first, any, now.t0, tid);      // (0 * NaN must not reach rows that do not see it)
+        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), phase ^ 1, kBarVEmpty)) return;
+        if (flags & kPageEdge) values.take_out_nan(first, any, now.t0, tid);      // (0 * NaN must not reach rows that do not see it)
         values.store(b.smem + L::kV + stage * L::kTile, tid);
         __syncwarp();
         if (lane == 0) {
             mbar_arrive(b.bar(kBarVFull + stage));
-            mbar_arrive(b.bar(kBarTileEmpty + turn));
+            mbar_arrive(b.bar(kBarPageEmpty + turn));
         }
         if (there) fetch_values(next);
-        ++it;
-        begins = flags & kTileLast;
+        ++page;
+        begins = flags & kPageLast;
         if (begins) ++seg;
     }
 }
@@ -613,19 +580,19 @@ __device__ __forceinline__ void store8(const AttnParams &p, int64_t at, const fl
 }
 
 template <int D>
-__device__ __forceinline__ void soften(const Block &b, int half, int r /* row of the half */, int lane) {
+__device__ __forceinline__ void soften(const Block &b, int r /* row of the tile */, int lane) {
     using L = Layout<D>;
     const AttnParams &p = b.p;
     Segments segments{b, L::kSegments};
     const uint32_t lanes = (uint32_t)(r & 96) << 16;
-    const uint32_t col_s = b.tmem + lanes + L::kColS + half * 128, col_o = b.tmem + lanes + L::kColO + half * D;
+    const uint32_t col_s = b.tmem + lanes + L::kColS, col_o = b.tmem + lanes + L::kColO;
     const float *const scales = reinterpret_cast<const float *>(b.smem + L::kScales);
-    uint32_t it = 0, pages = 0, seg = 0;
+    uint32_t pages = 0, seg = 0;
     for (;;) {
         const Segment *const at = segments.take();
         if (at == nullptr) break;
         const Segment &s = *at;
-        const int m = s.m0 + half * 128 + r, row = m / p.group, g = s.head * p.group + m - row * p.group;
+        const int m = s.m0 + r, row = m / p.group, g = s.head * p.group + m - row * p.group;
         const bool there = m < s.pairs;
         const int64_t q_at = (s.row0 + (int64_t)row) * p.q_row + g * p.q_head, out_at = (s.row0 + (int64_t)row) * p.out_row + g * p.out_head;
         if (s.flags & kEmptyItem) {
@@ -675,31 +642,31 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
                     else f = __half22float2(*reinterpret_cast<const __half2 *>(&u[x]));
                     h[x] = pack_f16x2(f.x * factor, f.y * factor);
                 }
-                *reinterpret_cast<uint4 *>(b.smem + L::kQ + half * L::kTile + (k >> 3) * L::kSlab + r * 128 + (((k & 7) ^ (r & 7)) << 4)) =
+                *reinterpret_cast<uint4 *>(b.smem + L::kQ + (k >> 3) * L::kQSlab + r * 128 + (((k & 7) ^ (r & 7)) << 4)) =
                     make_uint4(h[0], h[1], h[2], h[3]);
             }
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(b.bar(kBarQ + half));
+            if (lane == 0) mbar_arrive(b.bar(kBarQ));
         }
         const int lim = there ? min(s.hi, s.len - s.rows_all + row + 1) : s.hi;
         const int lim_min = __reduce_min_sync(0xffffffffu, lim);
-        const int lo = s.lo, n = (s.hi - s.t0 + kPage - 1) / kPage, start = s.t0;
+        const int lo = s.lo, n = s.pages, start = s.t0;
         float ref = kUnset, l = 0.f, unit = 0.f;
         bool ok = true;
         for (int u = 0; ok && u < n; ++u) {
-            const uint32_t tile = it + (u >> 1), page = pages + u, buffer = page & 1;
+            const uint32_t page = pages + u, buffer = page & 1;
             const uint32_t col = col_s + buffer * 64;
-            if ((u & 1) == 0) ok = warp_wait(b.ctx, b.bar(kBarScale + (tile & 3)), (tile >> 2) & 1, kBarScale);
+            ok = warp_wait(b.ctx, b.bar(kBarScale + (page & 3)), (page >> 2) & 1, kBarScale);
             if (!ok) break;
-            float a = back * scales[4 * (tile & 3) + (u & 1)];
-            const float vs = scales[4 * (tile & 3) + 2 + (u & 1)];
-            ok = warp_wait(b.ctx, b.bar(kBarS + 2 * half + buffer), (page >> 1) & 1, kBarS);
+            float a = back * scales[2 * (page & 3)];
+            const float vs = scales[2 * (page & 3) + 1];
+            ok = warp_wait(b.ctx, b.bar(kBarS + buffer), (page >> 1) & 1, kBarS);
             if (!ok) break;
             tcgen05_fence_after();
             // rescales O, once the MMAs of the page before are done with it
             auto shrink = [&](float factor) {
-                ok = warp_wait(b.ctx, b.bar(kBarO + 2 * half + (buffer ^ 1)), ((page - 1) >> 1) & 1, kBarO);
+                ok = warp_wait(b.ctx, b.bar(kBarO + (buffer ^ 1)), ((page - 1) >> 1) & 1, kBarO);
                 tcgen05_fence_after();
                 rescale<D>(col_o, factor);
             };
@@ -715,24 +682,25 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
             uint32_t w[32];
             uint64_t sum[4];
             for (int tries = 0;; ++tries) {
-                uint32_t v[2][32];
-                tmem_ld32(col, v[0]);
-                tmem_ld32(col + 32, v[1]);
-                tmem_wait_ld32(v[0]);
-                tmem_wait_ld32(v[1]);
                 const uint64_t a2 = pair(a, a), c2 = pair(-ref, -ref), f2 = pair(f, f);
                 float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) sum[k] = 0;
 #pragma unroll
-                for (int x = 0; x < 32; ++x) {
-                    float y0, y1, lo2, hi2;
-                    unpair(fma2(pair(__uint_as_float(v[x >> 4][2 * x & 31]), __uint_as_float(v[x >> 4][(2 * x & 31) + 1])), a2, c2), y0, y1);
-                    most[x & 3] = fmaxf(fmaxf(most[x & 3], y0), y1);
-                    const uint64_t e = pair(fast_exp2(y0), fast_exp2(y1));
-                    sum[x & 3] = add2(sum[x & 3], e);
-                    unpair(mul2(e, f2), lo2, hi2);
-                    w[x] = pack_f16x2(lo2, hi2);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t v[32];
+                    tmem_ld32(col + 32 * c, v);
+                    tmem_wait_ld32(v);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        float y0, y1, lo2, hi2;
+                        unpair(fma2(pair(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), a2, c2), y0, y1);
+                        most[x & 3] = fmaxf(fmaxf(most[x & 3], y0), y1);
+                        const uint64_t e = pair(fast_exp2(y0), fast_exp2(y1));
+                        sum[x & 3] = add2(sum[x & 3], e);
+                        unpair(mul2(e, f2), lo2, hi2);
+                        w[16 * c + x] = pack_f16x2(lo2, hi2);
+                    }
                 }
                 if (!__any_sync(0xffffffffu, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kLift + kSlack) || tries == 1) break;
                 const float top = largest_logit(col, a) - kLift;
@@ -749,18 +717,18 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
             tmem_wait_st();
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(b.bar(kBarP + 2 * half + buffer));
+            if (lane == 0) mbar_arrive(b.bar(kBarP + buffer));
         }
         if (!ok) return;
         // ---- epilogue
         const uint32_t end = pages + n - 1;
-        if (!warp_wait(b.ctx, b.bar(kBarO + 2 * half + (end & 1)), (end >> 1) & 1, kBarO)) return;
+        if (!warp_wait(b.ctx, b.bar(kBarO + (end & 1)), (end >> 1) & 1, kBarO)) return;
         tcgen05_fence_after();
         const float scale = l == 0.f ? 0.f : __fdividef(unit, l);
         const float lse2 = l == 0.f ? -INFINITY : ref + __log2f(l);
         const int *const nan = reinterpret_cast<const int *>(b.smem + L::kNan) + (seg & (kNanBuffers - 1)) * 128;
         const bool nans = reinterpret_cast<const volatile int *>(b.smem + L::kNanAny)[seg & (kNanBuffers - 1)] != 0;
-        float *const part = p.part_out + ((int64_t)s.slot * kTileRows + half * 128 + r) * D;
+        float *const part = p.part_out + ((int64_t)s.slot * kTileRows + r) * D;
 #pragma unroll 1
         for (int c = 0; c < D; c += 16) {
             float v[16];
@@ -786,10 +754,9 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
         }
         if (there) {
             if (s.slot < 0) p.lse[(s.row0 + (int64_t)row) * p.lse_row + g] = lse2 * kLn2;
-            else p.part_lse[s.slot * kTileRows + half * 128 + r] = lse2;
+            else p.part_lse[s.slot * kTileRows + r] = lse2;
         }
         tcgen05_fence_before();
-        it += s.tiles;
         pages += n;
         segments.done(lane);
         ++seg;
@@ -797,7 +764,7 @@ __device__ __forceinline__ void soften(const Block &b, int half, int r /* row of
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ splash_kv8_cache cache) {
     using L = Layout<D>;
     extern __shared__ uint8_t raw[];
@@ -809,13 +776,13 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
         for (int k = 0; k < 2; ++k) {
             mbar_init(bars + 8 * (kBarKFull + k), 4); mbar_init(bars + 8 * (kBarKEmpty + k), 1);
             mbar_init(bars + 8 * (kBarVFull + k), 4); mbar_init(bars + 8 * (kBarVEmpty + k), 1);
-            mbar_init(bars + 8 * (kBarQ + k), 4);
+            mbar_init(bars + 8 * (kBarS + k), 1); mbar_init(bars + 8 * (kBarP + k), 4); mbar_init(bars + 8 * (kBarO + k), 1);
         }
+        mbar_init(bars + 8 * kBarQ, 4);
         for (int k = 0; k < 4; ++k) {
             mbar_init(bars + 8 * (kBarScale + k), 1);
-            mbar_init(bars + 8 * (kBarS + k), 1); mbar_init(bars + 8 * (kBarP + k), 4); mbar_init(bars + 8 * (kBarO + k), 1);
-            mbar_init(bars + 8 * (kBarSegFull + k), 1); mbar_init(bars + 8 * (kBarSegEmpty + k), 9);
-            mbar_init(bars + 8 * (kBarTileFull + k), 1); mbar_init(bars + 8 * (kBarTileEmpty + k), 4);
+            mbar_init(bars + 8 * (kBarSegFull + k), 1); mbar_init(bars + 8 * (kBarSegEmpty + k), 5);
+            mbar_init(bars + 8 * (kBarPageFull + k), 1); mbar_init(bars + 8 * (kBarPageEmpty + k), 4);
         }
         misc[1] = 0;
         for (int k = 0; k < kNanBuffers; ++k) reinterpret_cast<int *>(smem + L::kNanAny)[k] = 0;
@@ -823,7 +790,7 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     }
     for (int k = tid; k < kNanBuffers * 128; k += kThreads) reinterpret_cast<int *>(smem + L::kNan)[k] = 0x7fffffff;
     if (warp == kWarpMma) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem + L::kMisc)), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem + L::kMisc)), "r"(L::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tcgen05_fence_before();
@@ -833,7 +800,7 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     grid_launch_dependents();
     const Share share = plan(p, worker);
     const Block b = {p, smem, smem_u32(smem), bars, misc[0], Ctx{misc + 1, p.status}};
-    if (warp < kWarpConvert) soften<D>(b, warp >> 2, tid & 127, lane);
+    if (warp < kWarpConvert) soften<D>(b, tid, lane);
     else if (warp < kWarpMma) convert<D>(b, tid - 32 * kWarpConvert, lane);
     else if (warp == kWarpMma) issue<D>(b, lane);
     else schedule<D>(b, cache, share, worker, lane);
@@ -846,7 +813,7 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     __syncthreads();
     if (warp == kWarpMma) {
         tcgen05_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(misc[0]), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(misc[0]), "r"(L::kColumns) : "memory");
     }
 }
 
@@ -865,6 +832,7 @@ cudaError_t launch_chunk(const AttnParams &p, const splash_kv8_cache &cache, cud
 cudaError_t launch_kv8_combine(const AttnParams &p, int D, int rows, int items, cudaStream_t stream);     // (of the decode path)
 
 int kv8_chunk_rows() { return kTileRows; }
+int kv8_chunk_workers(int sm_count) { return 2 * sm_count; }
 
 cudaError_t launch_kv8_chunk(const AttnParams &p, const splash_kv8_cache &cache, cudaStream_t stream) {
     cudaError_t e = cache.head_dim == 128 ? launch_chunk<128>(p, cache, stream) : launch_chunk<64>(p, cache, stream);

@@ -33,7 +33,7 @@ using namespace umma;
 
 constexpr int kConsumers = 4;                       // warps, 16 tokens of a page each
 constexpr int kThreads = 32 * (kConsumers + 1);
-constexpr int kOverhead = 2;                        // cost of an item beside its pages, in pages
+constexpr int kOverhead = 5;                        // cost of an item beside its pages, in pages (512 rollout requests: 98.5 us with 2, 96.5 with 4 to 6, 97.4 with 8)
 constexpr int kMinUnits = 2;                        // least cost of a worker's share
 
 enum { kFirst = 1, kLast = 2, kEmpty = 4, kEnd = 8, kEdge = 16, kCausal = 32 };
@@ -204,7 +204,7 @@ __device__ __forceinline__ void produce(const AttnParams &p, const Share &share,
         }
         a.row0 = r.row0; a.rows_all = r.rows_all; a.pairs = r.pairs; a.m0 = exists ? (sub % tiles) * L::kRows : 0;
         a.head = exists ? sub / tiles : 0; a.len = r.len; a.lo = r.lo; a.hi = r.hi;
-        a.slot = cut_front ? 2 * worker : cut_back ? 2 * worker + 1 : -1;
+        a.slot = pages == 0 ? -1 : cut_front ? 2 * worker : cut_back ? 2 * worker + 1 : -1;
         a.k_scale = valid ? p.k_scales[id * p.k_scale_stride + a.head] : 0.f;
         a.v_scale = valid ? p.v_scales[id * p.v_scale_stride + a.head] : 0.f;
         if (data) {
@@ -815,8 +815,8 @@ bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v
 
 // of the kernel for many rows
 cudaError_t launch_kv8_combine(const AttnParams &p, int D, int rows, int items, cudaStream_t stream) {
-    if (rows != 256) return cudaErrorInvalidValue;
-    return D == 128 ? launch_combine<128, 256>(p, items, stream) : launch_combine<64, 256>(p, items, stream);
+    if (rows != 128) return cudaErrorInvalidValue;
+    return D == 128 ? launch_combine<128, 128>(p, items, stream) : launch_combine<64, 128>(p, items, stream);
 }
 
 cudaError_t launch_kv8_decode(const AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
