@@ -97,21 +97,22 @@ View carve(void *base, int workers, int rows, int D) {
     return v;
 }
 
-// How a call runs: requests of up to kDecodePairs (row, head) pairs on the decode kernel, the others, if there may be any, on the kernel for chunks.
-// (A page and its 256 rows take the latter what three or four of the former's tiles take: where the two meet is measured at the constant.)
-constexpr int kDecodePairs = 64;
+// How a call runs: requests of up to this many (row, head) pairs on the decode kernel, the others, if there may be any, on the kernel for chunks, which
+// takes 128 pairs for about what the former takes for two of its tiles (64 contexts of 4,096 tokens, eight key heads of 128: 32 pairs 215 and 211 us, 64 pairs 411
+// and 217; of 64, whose tiles hold twice the pairs: 48 pairs 177 and 168, 32 pairs 132 and 167).
+int decode_pairs(const splash_kv8_cache *c) { return c->head_dim == 64 ? 48 : 32; }
 
 struct Plan { int rows, workers, chunk_workers; int64_t pairs; };
 
 Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
     Plan p;
     p.pairs = (int64_t)s->max_q_rows * (s->num_heads / c->num_kv_heads);
-    const int64_t pairs = p.pairs < kDecodePairs ? p.pairs : kDecodePairs;
+    const int64_t pairs = p.pairs < decode_pairs(c) ? p.pairs : decode_pairs(c);
     kv8_decode_shape(pairs, c->head_dim, sms, &p.rows, &p.workers);
     // no more blocks than the work can cost (with its overhead of five pages)
     const int64_t cost = (pairs + p.rows - 1) / p.rows * c->num_kv_heads * s->num_requests * (s->table_width + 5LL);
     if (cost > 0 && cost < p.workers) p.workers = (int)cost;
-    p.chunk_workers = p.pairs > kDecodePairs ? kv8_chunk_workers(sms) : 0;
+    p.chunk_workers = p.pairs > decode_pairs(c) ? kv8_chunk_workers(sms) : 0;
     return p;
 }
 
@@ -228,14 +229,14 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
     p.q_bf16 = query->dtype == SPLASH_DTYPE_BF16; p.out_f32 = query->out_dtype == SPLASH_DTYPE_FP32;
     p.whole = query->table_width <= kWholeRequestPages;
     p.workers = plan.workers;
-    p.min_pairs = 1; p.max_pairs = kDecodePairs;
+    p.min_pairs = 1; p.max_pairs = decode_pairs(cache);
     p.scale_log2 = query->softmax_scale * umma::kLog2e;
     p.status = v.status; p.cut = v.cut; p.part_lse = v.lse; p.part_out = v.out;
     cudaError_t e = launch_kv8_decode(p, cache->head_dim, plan.rows, k_map, v_map, static_cast<cudaStream_t>(stream));
     if (e == cudaSuccess && plan.chunk_workers > 0) {
         const View w = carve(workspace, plan.chunk_workers, kv8_chunk_rows(), cache->head_dim);
         p.workers = plan.chunk_workers;
-        p.min_pairs = kDecodePairs + 1; p.max_pairs = 0x7fffffff;
+        p.min_pairs = decode_pairs(cache) + 1; p.max_pairs = 0x7fffffff;
         p.cut = w.cut; p.part_lse = w.lse; p.part_out = w.out;
         e = launch_kv8_chunk(p, *cache, static_cast<cudaStream_t>(stream));
     }

@@ -135,16 +135,58 @@ __device__ __forceinline__ int64_t head_units(const AttnParams &p, const Request
     return n;
 }
 
+// The same by a warp, and the row tile that holds unit u of a key head (u becomes its unit of that tile).
+__device__ __forceinline__ int64_t head_units_warp(const AttnParams &p, const Request &r, int lane) {
+    int64_t n = 0;
+    const int tiles = row_tiles(p, r);
+    for (int t = lane; t < tiles; t += 32) n += kOverhead + tile_range(p, r, t).pages;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+    return n;
+}
+__device__ __forceinline__ int tile_of_unit(const AttnParams &p, const Request &r, int64_t &u, int lane) {
+    const int tiles = row_tiles(p, r);
+    for (int t0 = 0;; t0 += 32) {
+        const int cost = t0 + lane < tiles ? kOverhead + tile_range(p, r, t0 + lane).pages : 0;
+        int64_t sum = cost;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += x;
+        }
+        const unsigned behind = __ballot_sync(0xffffffffu, u < sum);      // tiles that end behind u
+        const int64_t all = __shfl_sync(0xffffffffu, sum, 31);
+        if (behind != 0 || t0 + 32 >= tiles) {
+            const int k = behind != 0 ? __ffs(behind) - 1 : 31;
+            u -= __shfl_sync(0xffffffffu, sum - cost, k);
+            return t0 + k;
+        }
+        u -= all;
+    }
+}
+
 struct Share { int64_t begin, end, total, u0; int i0, workers; };
 
 __device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
     __shared__ int64_t sums[kThreads / 32];
     __shared__ int64_t found_u;
     __shared__ int found_i;
+    // up to 40 requests: a warp works one's units out, a lane for each of its row tiles; more requests have fewer tiles: a thread each
+    constexpr int kFew = 40;
+    __shared__ int64_t units[kFew];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.B + kThreads - 1) / kThreads, i0 = min(tid * per, p.B), i1 = min(i0 + per, p.B);
+    const bool few = p.B <= kFew;
+    if (few) {
+        for (int i = warp; i < p.B; i += kThreads / 32) {
+            const int64_t n = p.kv_heads * head_units_warp(p, request(p, i), lane);
+            if (lane == 0) units[i] = n;
+        }
+        __syncthreads();
+    }
+    auto units_of = [&](int i) { return few ? units[i] : p.kv_heads * head_units(p, request(p, i)); };
     int64_t mine = 0;
-    for (int i = i0; i < i1; ++i) mine += p.kv_heads * head_units(p, request(p, i));
+    for (int i = i0; i < i1; ++i) mine += units_of(i);
     int64_t sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -168,7 +210,7 @@ __device__ __forceinline__ Share plan(const AttnParams &p, int worker) {
         int64_t u = s.begin - before;
         int i = i0;
         for (; i < i1; ++i) {
-            const int64_t n = p.kv_heads * head_units(p, request(p, i));
+            const int64_t n = units_of(i);
             if (u < n) break;
             u -= n;
         }
@@ -258,14 +300,10 @@ __device__ __forceinline__ void schedule(const Block &b, const splash_kv8_cache 
     int i = share.i0, head = 0, t = 0;
     if (i < p.B) {
         const Request r = request(p, i);
-        const int64_t per_head = head_units(p, r);
+        const int64_t per_head = head_units_warp(p, r, lane);
         head = (int)(share.u0 / per_head);
         int64_t u = share.u0 - head * per_head;
-        for (;; ++t) {
-            const int cost = kOverhead + tile_range(p, r, t).pages;
-            if (u < cost) break;
-            u -= cost;
-        }
+        t = tile_of_unit(p, r, u, lane);
         line -= u;                                   // where the item begins
     }
     while (ok && i < p.B && line < share.end) {
@@ -654,7 +692,13 @@ __device__ __forceinline__ void soften(const Block &b, int r /* row of the tile 
         const int lo = s.lo, n = s.pages, start = s.t0;
         float ref = kUnset, l = 0.f, unit = 0.f;
         bool ok = true;
-        for (int u = 0; ok && u < n; ++u) {
+        const bool idle = s.m0 + (r & 96) >= s.pairs;
+        for (int u = 0; idle && ok && u < n; ++u) {       // none of the warp's rows: what lies in their weights' place is as good as any
+            const uint32_t page = pages + u, buffer = page & 1;
+            ok = warp_wait(b.ctx, b.bar(kBarS + buffer), (page >> 1) & 1, kBarS);
+            if (ok && lane == 0) mbar_arrive(b.bar(kBarP + buffer));
+        }
+        for (int u = idle ? n : 0; ok && u < n; ++u) {
             const uint32_t page = pages + u, buffer = page & 1;
             const uint32_t col = col_s + buffer * 64;
             ok = warp_wait(b.ctx, b.bar(kBarScale + (page & 3)), (page >> 2) & 1, kBarScale);
