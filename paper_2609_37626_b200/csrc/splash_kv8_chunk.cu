@@ -3,7 +3,7 @@
 //
 // The (row, head) pairs of a request and key head, m = row * group + head, are cut in tiles of 128; an item of work is (request, key head, tile).
 // Two blocks of 10 warps share an SM, each with its own item, so that one's queries and outputs pass while the other works:
-//   - 4 converter warps read a page's codes (16 bytes a lane), widen them to fp16 (exact) and lay them out in shared memory, keys K-major and values
+//   - 4 converter warps, two for keys and two for values, read a page's codes (16 bytes a lane), widen them to fp16 (exact) and lay them out in shared memory, keys K-major and values
 //     MN-major in the 128-byte swizzle, two stages each;
 //   - 1 warp issues tcgen05.mma: S = Q K^T from shared memory into one of two buffers in tensor memory; O += P V with P read from tensor memory, where the
 //     softmax leaves it over S.  While the softmax has page u, S of page u + 1 is there and O of page u - 1 under way;
@@ -27,7 +27,7 @@ using namespace umma;
 constexpr int kTileRows = 128;
 constexpr int kOverhead = 6;                       // cost of an item beside its pages, in pages
 constexpr int kMinUnits = 8;                       // least cost of a worker's share
-constexpr int kWarpConvert = 4, kWarpMma = 8, kThreads = 32 * 10;      // (softmax 0 to 3, scheduler 9)
+constexpr int kWarpKeys = 4, kWarpValues = 6, kWarpMma = 8, kThreads = 32 * 10;      // (softmax 0 to 3, scheduler 9)
 constexpr int kNanBuffers = 8;
 
 enum { kEmptyItem = 1, kEndOfWork = 2 };
@@ -414,25 +414,25 @@ __device__ __forceinline__ void issue(const Block &b, int lane) {
     }
 }
 
-// Codes of one page's keys or values in registers on their way.  A lane has 16 bytes of rows `row` and row + 32 in each slab of 64 dimensions, row =
+// Codes of one page's keys or values in registers on their way.  Of two warps a lane has 16 bytes of the rows `row` + 16 k in each slab of 64 dimensions, row =
 // 8 warp + lane / 4: row mod 8, and with it the swizzle, is the same for all of them, and eight lanes' stores (four chunks of an even and of an odd
 // row) meet no bank twice.
 template <int D>
 struct Codes {
-    static constexpr int kSlabs = D / 64, kUnits = 2 * kSlabs;
+    static constexpr int kSlabs = D / 64, kUnits = 4 * kSlabs;
     uint4 w[kUnits];
     static __device__ __forceinline__ int row_of(int tid) { return (tid >> 5) * 8 + (tid >> 2 & 7); }
     // page NULL: zeros; edge: tokens outside [lo, hi) are zeros too
     __device__ __forceinline__ void load(const uint8_t *page, bool edge, int t0, int lo, int hi, int tid) {
         const int row = row_of(tid), at = row * D + (tid & 3) * 16;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int t = t0 + 32 * k + row;
+        for (int k = 0; k < 4; ++k) {
+            const int t = t0 + 16 * k + row;
             const bool there = page != nullptr && (!edge || (t >= lo && t < hi));
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) {
                 w[k * kSlabs + x] = make_uint4(0, 0, 0, 0);
-                if (there) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>(page + at + k * 32 * D + x * 64);
+                if (there) w[k * kSlabs + x] = *reinterpret_cast<const uint4 *>(page + at + k * 16 * D + x * 64);
             }
         }
     }
@@ -441,17 +441,17 @@ struct Codes {
         const int row = row_of(tid), unit = 2 * (tid & 3);
         uint8_t *const even = stage + row * 128 + ((unit ^ (row & 7)) << 4), *const odd = stage + row * 128 + (((unit + 1) ^ (row & 7)) << 4);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) {
                 const uint4 c = w[k * kSlabs + x];
                 uint4 h;
                 to_f16x4(c.x, h.x, h.y);
                 to_f16x4(c.y, h.z, h.w);
-                *reinterpret_cast<uint4 *>(even + x * Layout<D>::kSlab + k * 32 * 128) = h;
+                *reinterpret_cast<uint4 *>(even + x * Layout<D>::kSlab + k * 16 * 128) = h;
                 to_f16x4(c.z, h.x, h.y);
                 to_f16x4(c.w, h.z, h.w);
-                *reinterpret_cast<uint4 *>(odd + x * Layout<D>::kSlab + k * 32 * 128) = h;
+                *reinterpret_cast<uint4 *>(odd + x * Layout<D>::kSlab + k * 16 * 128) = h;
             }
     }
     // NaN codes become zeros; the first token with one is noted per dimension
@@ -464,7 +464,7 @@ struct Codes {
         if ((found & 0x80808080u) == 0) return;
         *any = 1;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int x = 0; x < kSlabs; ++x) {
                 const uint4 c = w[k * kSlabs + x];
@@ -474,66 +474,85 @@ struct Codes {
                     const uint32_t at = (((u[q] & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u;
                     u[q] &= ~(at * 0xffu);
                     for (int i = 0; i < 4; ++i)
-                        if (at >> (8 * i) & 1u) atomicMin(first + x * 64 + (tid & 3) * 16 + q * 4 + i, t0 + 32 * k + row_of(tid));
+                        if (at >> (8 * i) & 1u) atomicMin(first + x * 64 + (tid & 3) * 16 + q * 4 + i, t0 + 16 * k + row_of(tid));
                 }
                 w[k * kSlabs + x] = make_uint4(u[0], u[1], u[2], u[3]);
             }
     }
 };
 
+// The page behind `page` in the ring (NULL: no more work, or a wait gave up).
+__device__ __forceinline__ const Page *page_of_ring(const Block &b, uint32_t offset, uint32_t page) {
+    const bool ok = warp_wait(b.ctx, b.bar(kBarPageFull + (page & 3)), (page >> 2) & 1, kBarPageFull);
+    const Page *const t = reinterpret_cast<const Page *>(b.smem + offset) + (page & 3);
+    return ok && !(t->flags & kPageEnd) ? t : nullptr;
+}
+
+// Keys and values are converted by two warps each, so that a page's keys do not wait for the values of the one before.  Codes are fetched a page ahead.
 template <int D>
-__device__ __forceinline__ void convert(const Block &b, int tid, int lane) {
+__device__ __forceinline__ void convert_keys(const Block &b, int tid, int lane) {
     using L = Layout<D>;
-    int *const nan = reinterpret_cast<int *>(b.smem + L::kNan), *const nan_any = reinterpret_cast<int *>(b.smem + L::kNanAny);
     float *const scales = reinterpret_cast<float *>(b.smem + L::kScales);
-    const Page *const ring = reinterpret_cast<const Page *>(b.smem + L::kPages);
-    // codes are fetched a page ahead, keys behind the conversion of keys and values behind that of values
-    Codes<D> keys, values;
-    uint32_t page = 0, seg = 0;
-    bool begins = true;
-    if (!warp_wait(b.ctx, b.bar(kBarPageFull), 0, kBarPageFull)) return;
-    bool there = !(ring[0].flags & kPageEnd);
-    auto fetch_keys = [&](const Page &t) { keys.load(t.keys, t.flags & kPageEdge, t.t0, t.lo, t.hi, tid); };
-    auto fetch_values = [&](const Page &t) { values.load(t.values, t.flags & kPageEdge, t.t0, t.lo, t.hi, tid); };
-    if (there) { fetch_keys(ring[0]); fetch_values(ring[0]); }
-    while (there) {
-        const uint32_t stage = page & 1, turn = page & 3, phase = (page >> 1) & 1;
-        const Page &now = ring[turn], &next = ring[(page + 1) & 3];
-        const int flags = now.flags;
-        int *const first = nan + (seg & (kNanBuffers - 1)) * 128, *const any = nan_any + (seg & (kNanBuffers - 1));
-        if (begins) {         // a warp is at most two pages ahead of another, and the softmax warps at most two segments behind
-            nan[((seg + 2) & (kNanBuffers - 1)) * 128 + tid] = 0x7fffffff;
-            if (tid == 0) nan_any[(seg + 2) & (kNanBuffers - 1)] = 0;
-        }
-        if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), phase ^ 1, kBarKEmpty)) return;
-        keys.store(b.smem + L::kK + stage * L::kTile, tid);
-        const float vs = now.v_scale;
-        if ((flags & kPageEdge) && !isfinite(vs)) {      // every value of the page is NaN, for the rows that see a token of it
-            if (tid < D) atomicMin(first + tid, max(now.lo, now.t0));
-            *any = 1;
-        }
+    Codes<D> codes;
+    uint32_t page = 0;
+    const Page *now = page_of_ring(b, L::kPages, 0);
+    if (now != nullptr) codes.load(now->keys, now->flags & kPageEdge, now->t0, now->lo, now->hi, tid);
+    while (now != nullptr) {
+        const uint32_t stage = page & 1, turn = page & 3;
+        if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), ((page >> 1) & 1) ^ 1, kBarKEmpty)) return;
+        codes.store(b.smem + L::kK + stage * L::kTile, tid);
         if (tid == 0) {
-            scales[2 * turn] = now.k_scale;
-            scales[2 * turn + 1] = isfinite(vs) ? vs : flags & kPageEdge ? 0.f : NAN;
+            const float vs = now->v_scale;
+            scales[2 * turn] = now->k_scale;
+            scales[2 * turn + 1] = isfinite(vs) ? vs : now->flags & kPageEdge ? 0.f : NAN;
             mbar_arrive(b.bar(kBarScale + turn));
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(b.bar(kBarKFull + stage));
-        if (!warp_wait(b.ctx, b.bar(kBarPageFull + ((page + 1) & 3)), ((page + 1) >> 2) & 1, kBarPageFull)) return;
-        there = !(next.flags & kPageEnd);
-        if (there) fetch_keys(next);
-        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), phase ^ 1, kBarVEmpty)) return;
-        if (flags & kPageEdge) values.take_out_nan(first, any, now.t0, tid);      // (0 * NaN must not reach rows that do not see it)
-        values.store(b.smem + L::kV + stage * L::kTile, tid);
+        if (lane == 0) {
+            mbar_arrive(b.bar(kBarKFull + stage));
+            mbar_arrive(b.bar(kBarPageEmpty + turn));
+        }
+        now = page_of_ring(b, L::kPages, ++page);
+        if (now != nullptr) codes.load(now->keys, now->flags & kPageEdge, now->t0, now->lo, now->hi, tid);
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void convert_values(const Block &b, int tid, int lane) {
+    using L = Layout<D>;
+    int *const nan = reinterpret_cast<int *>(b.smem + L::kNan), *const nan_any = reinterpret_cast<int *>(b.smem + L::kNanAny);
+    Codes<D> codes;
+    bool begins = true;
+    uint32_t page = 0, seg = 0;
+    const Page *now = page_of_ring(b, L::kPages, 0);
+    if (now != nullptr) codes.load(now->values, now->flags & kPageEdge, now->t0, now->lo, now->hi, tid);
+    while (now != nullptr) {
+        const uint32_t stage = page & 1;
+        const int flags = now->flags;
+        if (begins) {         // a warp is at most two pages ahead of another, and the softmax warps at most two segments behind
+            int *const first = nan + ((seg + 2) & (kNanBuffers - 1)) * 128;
+            first[tid] = first[tid + 64] = 0x7fffffff;
+            if (tid == 0) nan_any[(seg + 2) & (kNanBuffers - 1)] = 0;
+        }
+        if (!warp_wait(b.ctx, b.bar(kBarVEmpty + stage), ((page >> 1) & 1) ^ 1, kBarVEmpty)) return;
+        if (flags & kPageEdge) {                     // 0 * NaN must not reach rows that do not see it
+            int *const first = nan + (seg & (kNanBuffers - 1)) * 128, *const any = nan_any + (seg & (kNanBuffers - 1));
+            codes.take_out_nan(first, any, now->t0, tid);
+            if (!isfinite(now->v_scale)) {           // every value of the page is NaN, for the rows that see a token of it
+                for (int d = tid; d < D; d += 64) atomicMin(first + d, max(now->lo, now->t0));
+                *any = 1;
+            }
+        }
+        codes.store(b.smem + L::kV + stage * L::kTile, tid);
         __syncwarp();
         if (lane == 0) {
             mbar_arrive(b.bar(kBarVFull + stage));
-            mbar_arrive(b.bar(kBarPageEmpty + turn));
+            mbar_arrive(b.bar(kBarPageEmpty + (page & 3)));
         }
-        if (there) fetch_values(next);
-        ++page;
         begins = flags & kPageLast;
         if (begins) ++seg;
+        now = page_of_ring(b, L::kPages, ++page);
+        if (now != nullptr) codes.load(now->values, now->flags & kPageEdge, now->t0, now->lo, now->hi, tid);
     }
 }
 
@@ -818,8 +837,8 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     const uint32_t bars = smem_u32(smem + L::kBars);
     if (tid == 0) {
         for (int k = 0; k < 2; ++k) {
-            mbar_init(bars + 8 * (kBarKFull + k), 4); mbar_init(bars + 8 * (kBarKEmpty + k), 1);
-            mbar_init(bars + 8 * (kBarVFull + k), 4); mbar_init(bars + 8 * (kBarVEmpty + k), 1);
+            mbar_init(bars + 8 * (kBarKFull + k), 2); mbar_init(bars + 8 * (kBarKEmpty + k), 1);
+            mbar_init(bars + 8 * (kBarVFull + k), 2); mbar_init(bars + 8 * (kBarVEmpty + k), 1);
             mbar_init(bars + 8 * (kBarS + k), 1); mbar_init(bars + 8 * (kBarP + k), 4); mbar_init(bars + 8 * (kBarO + k), 1);
         }
         mbar_init(bars + 8 * kBarQ, 4);
@@ -844,8 +863,9 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     grid_launch_dependents();
     const Share share = plan(p, worker);
     const Block b = {p, smem, smem_u32(smem), bars, misc[0], Ctx{misc + 1, p.status}};
-    if (warp < kWarpConvert) soften<D>(b, tid, lane);
-    else if (warp < kWarpMma) convert<D>(b, tid - 32 * kWarpConvert, lane);
+    if (warp < kWarpKeys) soften<D>(b, tid, lane);
+    else if (warp < kWarpValues) convert_keys<D>(b, tid - 32 * kWarpKeys, lane);
+    else if (warp < kWarpMma) convert_values<D>(b, tid - 32 * kWarpValues, lane);
     else if (warp == kWarpMma) issue<D>(b, lane);
     else schedule<D>(b, cache, share, worker, lane);
     if (misc[1]) {
