@@ -487,7 +487,7 @@ typedef struct splash_kv8_query {
     int64_t out_row_stride, out_head_stride;   /* multiples of 8 */
     int64_t lse_row_stride;
     int64_t block_table_stride;  /* entries from one request's row of block_table to the next */
-    int32_t table_width;         /* entries of a row that may be read: a context is cut at 64 * table_width tokens */
+    int32_t table_width;         /* entries of a row that may be read: a context is cut at 64 * table_width tokens (and at 2^30) */
     float softmax_scale;
 } splash_kv8_query;
 
@@ -505,7 +505,8 @@ typedef struct splash_kv8_query {
  * anything, NaN included; NaN in a token's data stays NaN in the rows that attend it.  A page id outside the
  * cache is never dereferenced, the page reads as zeros.  Products are exact (8-bit codes times q, which is scaled to fp16's range by a power of two per
  * row) and summed in fp32; softmax weights are rounded to fp16 relative to the row's running maximum, maxima and sums are
- * fp32.  Value scales that differ by up to 2^29 between the pages of a request keep that precision.  Results are bit-reproducible for a fixed call.
+ * fp32.  Value scales that differ by up to 2^20 between the pages of a request keep that precision.  Results are bit-reproducible for a fixed call.
+ * out and lse must not overlap each other, q or the cache.
  *
  *   block_table  [num_requests][block_table_stride] int32;  seq_lens, kv_begin, kv_end [num_requests] int32 (the latter two
  *                or NULL);  q_start [num_requests + 1] int32, ascending, or NULL
@@ -517,7 +518,8 @@ SPLASH_API int splash_kv8_attention(const splash_kv8_cache *cache, const splash_
                                     const int32_t *kv_begin, const int32_t *kv_end, void *out, float *lse,
                                     void *workspace, size_t workspace_bytes, void *stream);
 
-/* Workspace size for splash_kv8_attention (host computation); depends on head_dim and the device's SM count only.  Returns 0 on invalid arguments. */
+/* Workspace size for splash_kv8_attention (host computation, no device access); depends on the structs and the device's SM count.  Returns 0 on invalid
+ * arguments. */
 SPLASH_API size_t splash_kv8_attention_workspace_bytes(const splash_kv8_cache *cache, const splash_kv8_query *query);
 
 /* Host-side helpers. */

@@ -102,6 +102,8 @@ View carve(void *base, int workers, int rows, int D) {
 // and 217; of 64, whose tiles hold twice the pairs: 48 pairs 177 and 168, 32 pairs 132 and 167).
 int decode_pairs(const splash_kv8_cache *c) { return c->head_dim == 64 ? 48 : 32; }
 
+constexpr int64_t kMaxTokens = 1LL << 30;      // of a context: positions and page ends stay in 32 bits
+
 struct Plan { int rows, workers, chunk_workers; int64_t pairs; };
 
 Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
@@ -223,7 +225,7 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
     p.k_scales = cache->k_scales; p.v_scales = cache->v_scales;
     p.k_scale_stride = cache->k_scale_stride; p.v_scale_stride = cache->v_scale_stride;
     p.q_row = query->q_row_stride; p.q_head = query->q_head_stride; p.out_row = query->out_row_stride; p.out_head = query->out_head_stride;
-    p.lse_row = query->lse_row_stride; p.table_stride = query->block_table_stride; p.max_tokens = 64LL * query->table_width;
+    p.lse_row = query->lse_row_stride; p.table_stride = query->block_table_stride; p.max_tokens = 64LL * query->table_width < kMaxTokens ? 64LL * query->table_width : kMaxTokens;
     p.B = query->num_requests; p.T = (int32_t)query->num_rows; p.kv_heads = cache->num_kv_heads; p.group = query->num_heads / cache->num_kv_heads;
     p.num_pages = cache->num_pages; p.max_rows = query->max_q_rows;
     p.q_bf16 = query->dtype == SPLASH_DTYPE_BF16; p.out_f32 = query->out_dtype == SPLASH_DTYPE_FP32;

@@ -1,23 +1,27 @@
 // Attention of few query rows over a paged cache of keys and values in e4m3 with a scale per (page, head).
 //
-// For a key head the query rows of a request and the heads of the group form (row, head) pairs, m = row * group + head, cut in tiles of
-// 16 or 32.  An item of work is (request, key head, tile); its pages are streamed once:
+// For a key head the query rows of a request and the heads of the group form (row, head) pairs, m = row * group + head, cut in tiles of up to
+// 16 (heads of 64: 32).  An item of work is (request, key head, tile); its pages are streamed once:
 //     x = q . K * softmax_scale * log2 e * k_scale,  p = 2^(x - m + 7),  l += p,  O += p * v_scale / U * V
 // with a reference m per row that moves only when a logit exceeds it by 8 (then O and l are rescaled) and U the largest
-// value scale so far.  p <= 2^15 is rounded to fp16 for the product with V: 11 bits at any length of context, weights down to
-// 2^-29 of the largest one keep them.  Queries are scaled to fp16's range by a power of two per row, so that bf16 ones lose nothing.
+// value scale so far.  p <= 2^15 is rounded to fp16 for the product with V: 11 bits, for weights down to 2^-21 of the largest.  Queries are scaled to
+// fp16's range by a power of two per row, so that bf16 ones lose nothing.
 //
-// The cache's bytes bound it: 16 KB a page and head against 128 mma.m16n8k16.  What it takes to stay there:
+// The cache's bytes bound it, 16 KB a page and head of 128: one context of 262,144 tokens on eight key heads takes 92 us, 5.8 TB/s of the 6.5 that a copy
+// has; 64 contexts of 1k to 8k tokens 103 us, 5.9 TB/s; from 24 pairs on the MMAs and conversions do (heads of 128, 64 contexts of 4,096 tokens: 8 pairs 92 us,
+// 16 pairs 118, 24 and 32 pairs 212).  What it takes to stay there:
 //   - items are cut where the cost line (pages, and kOverhead per item) of all requests passes a worker's share, so one long
-//     context and 512 short ones fill the SMs alike; cut items are joined by a combine kernel.  Two workers per SM.
+//     context and 512 short ones fill the SMs alike; cut items are joined by a combine kernel.  Three workers per SM;
 //   - a producer warp walks the line, 32 pages at once: a lane each finds its page, its scales and its flags; TMA brings
-//     keys and values (swizzled against bank conflicts), four or eight pages ahead, across items;
+//     keys and values (swizzled against bank conflicts), three or six pages ahead, across items;
 //   - four warps take 16 tokens of every page each, with their own m, l, O: they meet only at the end of an item;
+//   - tokens and dimensions are the MMAs' m, rows their n: eight rows fill it (rows on m, 16 at a time, were half empty: the same contexts took 128 and 143 us);
+//     weights are turned from S's layout to the operand's by movmatrix;
 //   - the order of dimensions within an MMA's k does not matter if both operands agree, nor the order of tokens: a lane reads
 //     its key and value codes 16 bytes at a time and widens them in registers (e4m3 -> fp16 is exact).  Keys: lane (n, c) of the fragment takes
 //     token perm(n) and the 16-byte chunks c, c + 4 of its row, which are the values of the k slots 2c, 2c + 1, 2c + 8, 2c + 9 of successive
 //     MMAs; values: tokens c, c + 4, c + 8, c + 12 and the chunk perm(n), bytes of two tokens interleaved.
-// mma.sync and not tcgen05: with at most 32 rows the MMAs take a fifth of the time that the bytes take, and the 8-bit
+// mma.sync and not tcgen05: with so few rows the MMAs take a third of the time that the bytes take, and the 8-bit
 // operands would have to be widened into shared memory first, twice the bytes over the path that is next in line.
 #include <type_traits>
 
@@ -802,7 +806,9 @@ cudaError_t launch_decode(const AttnParams &p, int items, const CUtensorMap &k_m
 
 }  // namespace
 
-// Rows of a tile for requests of at most `pairs` (row, head) pairs, and the workers that the line is cut for (the blocks that the GPU holds).
+// Rows of a tile for requests of at most `pairs` (row, head) pairs, and the workers that the line is cut for (the blocks that the GPU holds).  More rows
+// than 16 of 128 dimensions do not fit the registers of three blocks an SM (32: 47 us where two tiles of 16 take 37); of 64 dimensions 24 rows as one tile
+// take 37 us, as two of 16 as much, 32 rows 132 as one tile and 146 as two.
 void kv8_decode_shape(int64_t pairs, int head_dim, int sm_count, int *rows, int *workers) {
     const int64_t most = head_dim == 64 ? 32 : 16, tiles = (pairs + most - 1) / most;
     *rows = (int)((pairs + tiles - 1) / tiles + 7) / 8 * 8;

@@ -252,3 +252,49 @@ def test_head_slices_of_shared_buffers():
         B.splash_kv8_attention(q.cuda()[:, 3 * a:3 * b], ck[:, a:b], cv[:, a:b], ks[:, a:b], vs[:, a:b], table, lens, softmax_scale=0.125, out=out[:, 3 * a:3 * b],
                                lse=lse[:, 3 * a:3 * b])
     _kv8.check((out.double().cpu().numpy(), lse.cpu().numpy()), _kv8.attention(cache, q.double().numpy(), None, 0.125, out_eps=2.0 ** -8))
+
+
+@pytest.mark.parametrize("rows", [None, [70, 40]])
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1e-30])
+def test_odd_softmax_scales(rows, scale):
+    cache = _kv8.Cache(24, [200, 90], 2, 128)
+    attend(cache, queries(24, 2 if rows is None else sum(rows), 8, 128, "bf16"), rows, scale=scale)
+
+
+@pytest.mark.parametrize("rows", [None, [50, 90]])
+def test_a_table_without_columns(rows):
+    cache = _kv8.Cache(25, [200, 90], 2, 64)
+    cache.table = np.zeros((2, 0), np.int32)
+    out, lse = attend(cache, queries(25, 2 if rows is None else sum(rows), 4, 64, "fp16"), rows, "fp16")
+    assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+def test_requests_without_tokens_anywhere_on_the_line():
+    # many empty requests between long ones: wherever the work is cut, their outputs are written where they belong
+    for D, group in ((64, 1), (128, 4), (128, 16)):
+        lens = [0, 0, 3000, 0, 1, 0, 0, 0, 2000] + [0] * 60 + [700, 0]
+        cache = _kv8.Cache([26, D], lens, 1, D)
+        attend(cache, queries(26, len(lens), group, D, "bf16"), None)
+
+
+def test_many_key_heads_and_wide_groups():
+    cache = _kv8.Cache(27, [130, 70], 33, 64)
+    attend(cache, queries(27, 2, 33, 64, "bf16"), None)
+    cache = _kv8.Cache(28, [300, 5], 1, 128)
+    attend(cache, queries(28, 2, 128, 128, "bf16"), None)
+    attend(cache, queries(28, 6, 200, 128, "fp16"), [4, 2], "fp16")
+
+
+def test_chunks_cut_and_joined():
+    # few tiles over long contexts: pages of one tile are spread over many workers
+    for D, rows, lens, kv in ((128, [200], [20000], 1), (64, [40, 3], [30000, 9000], 2)):
+        cache = _kv8.Cache([29, D], lens, kv, D)
+        attend(cache, queries(29, sum(rows), 4 * kv, D, "bf16"), rows)
+
+
+def test_a_batch_of_many_chunks():
+    g = np.random.default_rng(30)
+    rows = [int(v) for v in g.integers(0, 70, 90)]
+    lens = [r + int(v) for r, v in zip(rows, g.integers(0, 300, 90))]
+    cache = _kv8.Cache(30, lens, 1, 64)
+    attend(cache, queries(30, sum(rows), 2, 64, "bf16"), rows)
