@@ -44,11 +44,12 @@ enum { kFirst = 1, kLast = 2, kEmpty = 4, kEnd = 8, kEdge = 16, kCausal = 32 };
 
 // What the consumers need to know about a page in the ring, written by the producer.
 struct alignas(16) PageInfo {
+    int flags;                          // (these four are read at once, for every page)
+    float k_scale, v_scale;
+    int t0;                             // first token of the page
     int row0, rows_all, pairs, m0;      // the item's rows
     int head, len, lo, hi;              // key head; context; the request's token range
-    int t0, flags, slot, pad;           // first token of the page; partial slot or -1
-    float k_scale, v_scale;
-    int pad2[2];
+    int slot, pad[3];                   // partial slot or -1
 };
 
 // NT: tiles of eight rows
@@ -319,7 +320,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
     const int tok_a = D == 128 ? c : 2 * c, tok_b = D == 128 ? c + 4 : 2 * c + 1;
     const int tok[4] = {tok_a, tok_b, tok_a + 8, tok_b + 8};
 
-    float o[NT][kM][4], ref[NT][2], l[NT][2], rs[NT][2], unit = 0.f;      // of the rows 2c, 2c + 1 of each tile of eight
+    float o[NT][kM][4], ref[NT][2], l[NT][2], rs[NT][2], unit = 0.f, per_unit = 0.f;      // of the rows 2c, 2c + 1 of each tile of eight
     uint32_t qf[kQueryShared ? 1 : NT][kK][2];
     int lim[NT][2];
     int stage = 0;
@@ -327,7 +328,8 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
     for (;;) {
         if (!warp_wait(ctx, full + 8 * stage, phase, 140 + stage)) break;
         const PageInfo &info = infos[stage];
-        const int flags = info.flags;
+        const int4 page = *reinterpret_cast<const int4 *>(&info);
+        const int flags = page.x;
         if (flags & kEnd) break;
         if (flags & (kFirst | kEmpty)) {
             // the item's queries, as fp16 with a power of two per row that brings the largest of a row to [2^14, 2^15)
@@ -372,7 +374,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
 #pragma unroll
                     for (int x = 0; x < 4; ++x) o[nt][j][x] = 0.f;
             }
-            unit = 0.f;
+            unit = per_unit = 0.f;
             if (kQueryShared && !meet(ctx, group_bar, group_phase, lane)) break;
         }
         if (!(flags & kEmpty)) {
@@ -419,9 +421,10 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                 }
             }
             // ---- weights, in base 2 relative to the row's reference, and relative to the largest value scale so far
-            const float ks = info.k_scale, vs = isinf(info.v_scale) ? NAN : info.v_scale;
+            const float ks = __int_as_float(page.y), scale = __int_as_float(page.z), vs = fabsf(scale) == INFINITY ? NAN : scale;
             if (fabsf(vs) > unit) {
-                const float a = __fdividef(unit, fabsf(vs));
+                per_unit = __fdividef(1.f, fabsf(vs));
+                const float a = unit * per_unit;
                 unit = fabsf(vs);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -430,10 +433,10 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
 #pragma unroll
                         for (int x = 0; x < 4; ++x) o[nt][j][x] *= a;
             }
-            const float f = vs == unit ? 1.f : __fdividef(vs, unit);
+            const float f = vs == unit ? 1.f : vs * per_unit;
             uint32_t hidden = 0;                     // logits of tokens that the row does not see, a bit each
             if (flags & kEdge) {
-                const int base = info.t0 + 16 * warp, lo = info.lo, hi = info.hi;
+                const int base = page.w + 16 * warp, lo = info.lo, hi = info.hi;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -448,7 +451,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                         for (int q = 0; q < D / 32; ++q) vw[t][q] = 0;
                     }
             }
-            float y[NT][4], most = -INFINITY;
+            float y[NT][4], most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             auto relative = [&] {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -466,8 +469,8 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) most = fmaxf(most, y[nt][x]);
-            if (__any_sync(0xffffffffu, most > kLift + kSlack)) {
+                for (int x = 0; x < 4; ++x) most[x] = fmaxf(most[x], y[nt][x]);
+            if (__any_sync(0xffffffffu, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kLift + kSlack)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
