@@ -38,6 +38,7 @@ struct AttnParams {
     int32_t q_bf16, out_f32;
     int32_t whole;                    // 1: no piece of work is cut, and no combine kernel follows
     int32_t workers;
+    int32_t clear_status;             // 1: no kernel of the call in front has cleared the error words (the decode kernel does)
     int32_t min_pairs, max_pairs;     // requests with this many (row, head of the group) pairs are this kernel's
     float scale_log2;                 // softmax scale times log2 e
     // workspace

@@ -98,13 +98,13 @@ View carve(void *base, int workers, int rows, int D) {
 }
 
 // How a call runs: requests of up to this many (row, head) pairs on the decode kernel, the others, if there may be any, on the kernel for chunks, which
-// takes 128 pairs for about what the former takes for two of its tiles (64 contexts of 4,096 tokens, eight key heads of 128: 32 pairs 215 and 211 us, 64 pairs 411
-// and 217; of 64, whose tiles hold twice the pairs: 48 pairs 177 and 168, 32 pairs 132 and 167).
-int decode_pairs(const splash_kv8_cache *c) { return c->head_dim == 64 ? 48 : 32; }
+// takes 128 pairs for about what the former takes for two of its tiles (64 contexts of 4,096 tokens, eight key heads of 128: 32 pairs 218 and 188 us, but four of them 27 and 30, 64 pairs 411
+// and 191; of 64, whose tiles hold twice the pairs: 48 pairs 178 and 143, 32 pairs 134 and about as much).
+int decode_pairs(const splash_kv8_cache *c) { return c->head_dim == 64 ? 40 : 32; }
 
 constexpr int64_t kMaxTokens = 1LL << 30;      // of a context: positions and page ends stay in 32 bits
 
-struct Plan { int rows, workers, chunk_workers; int64_t pairs; };
+struct Plan { int rows, workers, chunk_workers; int64_t pairs; bool decode; };
 
 Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
     Plan p;
@@ -115,6 +115,9 @@ Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
     const int64_t cost = (pairs + p.rows - 1) / p.rows * c->num_kv_heads * s->num_requests * (s->table_width + 5LL);
     if (cost > 0 && cost < p.workers) p.workers = (int)cost;
     p.chunk_workers = p.pairs > decode_pairs(c) ? kv8_chunk_workers(sms) : 0;
+    // With T rows in all and at most R for a request, at most (B R - T) / (R - 1) requests have a single one.  Where that is a quarter of them or less (a step of
+    // a fixed number of rows, one prompt), the kernel for chunks takes them all: two launches less, 6 us of such a call.
+    p.decode = p.chunk_workers == 0 || (int64_t)s->num_requests * s->max_q_rows - s->num_rows > (s->max_q_rows - 1LL) * s->num_requests / 4;
     return p;
 }
 
@@ -217,7 +220,7 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
         return SPLASH_INVALID_ARG;
     }
     CUtensorMap k_map, v_map;
-    if (!kv8_pool_maps(*cache, &k_map, &v_map)) return SPLASH_CUDA_ERROR;
+    if (plan.decode && !kv8_pool_maps(*cache, &k_map, &v_map)) return SPLASH_CUDA_ERROR;
     kv8::AttnParams p;
     memset(&p, 0, sizeof p);
     p.q = q; p.out = out; p.lse = lse;
@@ -234,11 +237,12 @@ int splash_kv8_attention(const splash_kv8_cache *cache, const splash_kv8_query *
     p.min_pairs = 1; p.max_pairs = decode_pairs(cache);
     p.scale_log2 = query->softmax_scale * umma::kLog2e;
     p.status = v.status; p.cut = v.cut; p.part_lse = v.lse; p.part_out = v.out;
-    cudaError_t e = launch_kv8_decode(p, cache->head_dim, plan.rows, k_map, v_map, static_cast<cudaStream_t>(stream));
+    cudaError_t e = plan.decode ? launch_kv8_decode(p, cache->head_dim, plan.rows, k_map, v_map, static_cast<cudaStream_t>(stream)) : cudaSuccess;
     if (e == cudaSuccess && plan.chunk_workers > 0) {
         const View w = carve(workspace, plan.chunk_workers, kv8_chunk_rows(), cache->head_dim);
         p.workers = plan.chunk_workers;
-        p.min_pairs = decode_pairs(cache) + 1; p.max_pairs = 0x7fffffff;
+        p.clear_status = !plan.decode;
+        p.min_pairs = plan.decode ? decode_pairs(cache) + 1 : 1; p.max_pairs = 0x7fffffff;
         p.cut = w.cut; p.part_lse = w.lse; p.part_out = w.out;
         e = launch_kv8_chunk(p, *cache, static_cast<cudaStream_t>(stream));
     }

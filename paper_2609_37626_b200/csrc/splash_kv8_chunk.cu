@@ -861,6 +861,7 @@ kv8_chunk_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ s
     tcgen05_fence_after();
     grid_dependency_wait();
     grid_launch_dependents();
+    if (p.clear_status && blockIdx.x == 0 && tid < 4) p.status[tid] = 0;
     const Share share = plan(p, worker);
     const Block b = {p, smem, smem_u32(smem), bars, misc[0], Ctx{misc + 1, p.status}};
     if (warp < kWarpKeys) soften<D>(b, tid, lane);
