@@ -8,7 +8,6 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
-#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -677,13 +676,15 @@ PyObject *kv8_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyO
     s.q_row_stride = q.stride(0); s.q_head_stride = q.stride(1); s.out_row_stride = out.stride(0); s.out_head_stride = out.stride(1);
     s.lse_row_stride = lse.stride(0); s.block_table_stride = table.stride(0); s.table_width = (int32_t)table.size(1);
     s.softmax_scale = (float)scale;
-    // Scratch for this call alone, given back to the allocator behind it: calls on two streams, or in two captured graphs, share none.
+    // Scratch for this call alone, of the call's stream: calls on two streams, or in two captured graphs, share none, and no work that another stream
+    // still has before it reaches it.
     at::Tensor scratch;
     if (ws == nullptr) {
         const size_t need = splash_kv8_attention_workspace_bytes(&cache, &s);
         if (need == 0) return raise_status(splash_kv8_attention(&cache, &s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, stream));
+        c10::cuda::OptionalCUDAStreamGuard on;
+        if (given(o[15])) on.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, q.device().index()));
         scratch = new_tensor({(int64_t)need}, at::kByte, q);
-        if (given(o[15])) c10::cuda::CUDACachingAllocator::recordStream(scratch.storage().data_ptr(), c10::cuda::getStreamFromExternal((cudaStream_t)stream, q.device().index()));
     } else {
         scratch = *ws;
         SPLASH_ASSERT(scratch.is_contiguous());

@@ -149,3 +149,24 @@ def test_places_for_the_latent_cache():
     a = dw.decode()
     b = B.splash_mla_decode(dw.q, pool, table, after, softmax_scale=w.softmax_scale)
     assert (a[0] - b[0]).abs().max() <= 1e-2 and (a[1] - b[1]).abs().max() <= 1e-3
+
+
+def test_scratch_belongs_to_the_given_stream():
+    """Memory of the current stream's pool may still be in use by what that stream has before it, which the given stream does not wait for."""
+    cache = _kv8.Cache([3], [700, 4000], 2, 128)
+    tensors = cache.cuda()
+    q = torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(2, 8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def allocated(stream):
+        return sum(s["allocated_size"] + s["total_size"] for s in torch.cuda.memory_snapshot() if s["stream"] == stream.cuda_stream)
+
+    here, there = allocated(torch.cuda.current_stream()), allocated(side)
+    with torch.cuda.stream(torch.cuda.default_stream()):
+        B.splash_kv8_attention(q, *tensors, softmax_scale=1.0, out=out, lse=lse, stream=side)
+    assert allocated(side) > there and allocated(torch.cuda.current_stream()) == here
+    B.splash_kv8_attention(q, *tensors, softmax_scale=1.0, out=out, lse=lse, stream=torch.cuda.default_stream())
+    torch.cuda.synchronize()
+    assert torch.isfinite(lse).all()
