@@ -636,6 +636,56 @@ __device__ __forceinline__ void store8(const AttnParams &p, int64_t at, const fl
     }
 }
 
+// The warp's rows of a finished segment, from tensor memory to out or to the workspace; out of line, which leaves the main loop its registers.  Rows of 16-bit
+// outputs go through the place of the segment's queries, which no MMA reads any more and of which each warp has that of its own rows, so that lanes side by
+// side write consecutive memory (two prompt chunks of 2,048 rows behind 8,192 tokens, 32 heads on 8 of 128: 517 us; inline, 16 bytes of a row a lane: 559).  A
+// lane has 64 bytes of an fp32 row at a time, which are whole sectors as they are (by way of shared memory 523).
+template <int D>
+__device__ __noinline__ void give(const Block &b, const Segment &s, int r, int lane, uint32_t col_o, float scale, const int *nan, int lim) {
+    const AttnParams &p = b.p;
+    const int m = s.m0 + r, row = m / p.group, g = s.head * p.group + m - row * p.group;
+    const bool there = m < s.pairs, wide = s.slot >= 0 || p.out_f32 != 0;
+    const int64_t out_at = (s.row0 + (int64_t)row) * p.out_row + g * p.out_head;
+    float *const out32 = s.slot < 0 ? static_cast<float *>(p.out) + out_at : p.part_out + ((int64_t)s.slot * kTileRows + r) * D;
+    auto place = [&](int row, int k) {                // 16 bytes of it
+        return reinterpret_cast<uint4 *>(b.smem + Layout<D>::kQ + (k >> 3) * Layout<D>::kQSlab + row * 128 + (((k & 7) ^ (row & 7)) << 4));
+    };
+#pragma unroll 1
+    for (int c = 0; c < D; c += 16) {
+        float v[16];
+        tmem_ld16(col_o + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            v[x] *= scale;
+            if (nan != nullptr && nan[c + x] < lim) v[x] = NAN;
+        }
+        if (wide) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (there) reinterpret_cast<float4 *>(out32 + c)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float *const u = v + 8 * k;
+                *place(r, c / 8 + k) = p.q_bf16 ? make_uint4(pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]), pack_bf16x2(u[4], u[5]), pack_bf16x2(u[6], u[7]))
+                                                : make_uint4(pack_f16x2(u[0], u[1]), pack_f16x2(u[2], u[3]), pack_f16x2(u[4], u[5]), pack_f16x2(u[6], u[7]));
+            }
+        }
+    }
+    if (wide) return;
+    __syncwarp();
+    constexpr int kLanes = D / 8;                     // of a row
+#pragma unroll 4
+    for (int k = 0; k < kLanes; ++k) {
+        const int from = k * (32 / kLanes) + lane / kLanes;
+        const int64_t to = __shfl_sync(0xffffffffu, there ? out_at : -1, from);
+        const uint4 x = *place((r & 96) + from, lane % kLanes);
+        if (to >= 0) *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p.out) + to + 8 * (lane % kLanes)) = x;
+    }
+    __syncwarp();                                     // the next segment's queries are written behind these reads
+}
+
 template <int D>
 __device__ __forceinline__ void soften(const Block &b, int r /* row of the tile */, int lane) {
     using L = Layout<D>;
@@ -791,30 +841,7 @@ __device__ __forceinline__ void soften(const Block &b, int r /* row of the tile 
         const float lse2 = l == 0.f ? -INFINITY : ref + __log2f(l);
         const int *const nan = reinterpret_cast<const int *>(b.smem + L::kNan) + (seg & (kNanBuffers - 1)) * 128;
         const bool nans = reinterpret_cast<const volatile int *>(b.smem + L::kNanAny)[seg & (kNanBuffers - 1)] != 0;
-        float *const part = p.part_out + ((int64_t)s.slot * kTileRows + r) * D;
-#pragma unroll 1
-        for (int c = 0; c < D; c += 16) {
-            float v[16];
-            tmem_ld16(col_o + c, v);
-            tmem_wait_ld();
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                v[x] *= scale;
-                if (nans && nan[c + x] < lim) v[x] = NAN;
-            }
-            if (there) {
-                if (s.slot < 0) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float u[8] = {v[8 * k], v[8 * k + 1], v[8 * k + 2], v[8 * k + 3], v[8 * k + 4], v[8 * k + 5], v[8 * k + 6], v[8 * k + 7]};
-                        store8(p, out_at + c + 8 * k, u);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) reinterpret_cast<float4 *>(part + c)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-                }
-            }
-        }
+        give<D>(b, s, r, lane, col_o, scale, nans ? nan : nullptr, lim);
         if (there) {
             if (s.slot < 0) p.lse[(s.row0 + (int64_t)row) * p.lse_row + g] = lse2 * kLn2;
             else p.part_lse[s.slot * kTileRows + r] = lse2;
