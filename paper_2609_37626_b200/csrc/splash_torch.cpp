@@ -513,6 +513,15 @@ bool stream_on(PyObject *o, c10::DeviceIndex device, void *&stream) {
     return stream_of(o, stream);
 }
 
+// While it lives, memory for a call on a given stream comes from that stream's pool: the current stream may still have work before it that
+// uses what its own pool hands out, and the given stream waits for none of it.
+struct MemoryOf {
+    c10::cuda::OptionalCUDAStreamGuard on;
+    MemoryOf(PyObject *o, void *stream, c10::DeviceIndex device) {
+        if (given(o)) on.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, device));
+    }
+};
+
 // A 1-D tensor over a part of another one's memory.
 at::Tensor part_of(const at::Tensor &all, int64_t byte, int64_t n, at::ScalarType dtype) {
     at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(dtype));
@@ -543,6 +552,9 @@ PyObject *kv_slots(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject
     SPLASH_ASSERT(places >= 0);
     if (!on_one_gpu({table, lens, more, free_pages, begin, given_out[0], given_out[1], given_out[2], given_out[3], given_out[4]})) return nullptr;
     const c10::cuda::CUDAGuard guard(table->device());
+    void *stream;
+    if (!stream_on(v[11], table->device().index(), stream)) return nullptr;
+    const MemoryOf memory(v[11], stream, table->device().index());
     const int64_t sizes[5] = {places, places, B + 1, B, 4};
     at::Tensor out[5], all;
     int64_t bytes = 0, at[5];
@@ -554,8 +566,6 @@ PyObject *kv_slots(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject
         out[k] = *given_out[k];
         SPLASH_ASSERT(out[k].dim() == 1 && out[k].numel() == sizes[k] && out[k].is_contiguous() && out[k].scalar_type() == (k == 0 ? at::kLong : at::kInt));
     }
-    void *stream;
-    if (!stream_on(v[11], table->device().index(), stream)) return nullptr;
     void *const table_at = table->data_ptr(), *const slot_at = out[0].data_ptr(), *const pos_at = out[1].data_ptr(), *const start_at = out[2].data_ptr(),
                *const after_at = out[3].data_ptr(), *const counts_at = out[4].data_ptr();
     const void *const lens_at = lens->data_ptr(), *const more_at = more->data_ptr(), *const free_at = free_pages->data_ptr(), *const begin_at = begin->data_ptr();
@@ -664,6 +674,7 @@ PyObject *kv8_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyO
     const c10::cuda::CUDAGuard guard(q.device());
     void *stream;
     if (!stream_on(o[15], q.device().index(), stream)) return nullptr;
+    const MemoryOf memory(o[15], stream, q.device().index());
     at::Tensor out, lse;
     if (given_out) out = *given_out; else out = new_tensor({q.size(0), q.size(1), q.size(2)}, q.scalar_type(), q);
     if (given_lse) lse = *given_lse; else lse = new_tensor({q.size(0), q.size(1)}, at::kFloat, q);
@@ -676,14 +687,11 @@ PyObject *kv8_attention(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyO
     s.q_row_stride = q.stride(0); s.q_head_stride = q.stride(1); s.out_row_stride = out.stride(0); s.out_head_stride = out.stride(1);
     s.lse_row_stride = lse.stride(0); s.block_table_stride = table.stride(0); s.table_width = (int32_t)table.size(1);
     s.softmax_scale = (float)scale;
-    // Scratch for this call alone, of the call's stream: calls on two streams, or in two captured graphs, share none, and no work that another stream
-    // still has before it reaches it.
+    // Scratch for this call alone: calls on two streams, or in two captured graphs, share none.
     at::Tensor scratch;
     if (ws == nullptr) {
         const size_t need = splash_kv8_attention_workspace_bytes(&cache, &s);
         if (need == 0) return raise_status(splash_kv8_attention(&cache, &s, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, stream));
-        c10::cuda::OptionalCUDAStreamGuard on;
-        if (given(o[15])) on.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, q.device().index()));
         scratch = new_tensor({(int64_t)need}, at::kByte, q);
     } else {
         scratch = *ws;
@@ -770,7 +778,8 @@ PyMethodDef kMethods[] = {
      "Places of a step's new tokens, from the lengths on the device; see splash_kv_slots in include/splash_mla.h.\n\n"
      "block_table [B][width] int32 gets the ids of new pages, in place; seq_lens, new_lens [B], free_pages [F],\n"
      "free_begin [1] int32.  Returns (slot_map [num_slots] int64, positions [num_slots], q_start [B + 1],\n"
-     "new_seq_lens [B], counts [4] int32: places asked for, pages taken, requests refused, the next free_begin).\n"},
+     "new_seq_lens [B], counts [4] int32: places asked for, pages taken, requests refused, the next free_begin).\n"
+     "Outputs that are not given are allocated for the call's stream.\n"},
     {"splash_kv8_append", FAST(kv8_append), METH_FASTCALL | METH_KEYWORDS,
      "splash_kv8_append(k, v, slot_map, k_pool, v_pool, k_scales, v_scales, *, stream=None)\n--\n\n"
      "Write keys and values into an e4m3 cache, in place; see splash_kv8_append in include/splash_mla.h.\n\n"
@@ -782,7 +791,8 @@ PyMethodDef kMethods[] = {
      "Causal attention of each request's newest rows over an e4m3 cache; see splash_kv8_attention in include/splash_mla.h.\n\n"
      "q [T][H][D] bf16 or fp16, rows q_start[i] .. q_start[i + 1] - 1 belong to request i (None: row i), at most max_q_rows each;\n"
      "pools and scales as for splash_kv8_append, H a multiple of their heads; block_table [B][width], seq_lens, kv_begin, kv_end [B] int32.\n"
-     "Returns (out [T][H][D] of q's type, or the given fp32 tensor; lse [T][H] fp32).\n"},
+     "Returns (out [T][H][D] of q's type, or the given fp32 tensor; lse [T][H] fp32).  What is not given (outputs, workspace) is\n"
+     "allocated for the call's stream.\n"},
     {"set_error_class", set_error_class, METH_O, "The exception class of a call that did not succeed."},
     {"cached_workspace", cached, METH_VARARGS, "The scratch buffer that calls without one share on a device, or None."},
     {nullptr, nullptr, 0, nullptr}};
