@@ -127,6 +127,21 @@ at::Tensor new_tensor(at::IntArrayRef size, at::ScalarType dtype, const at::Tens
     return at::Tensor(at::detail::empty_cuda(size, dtype, like.device(), std::nullopt));
 }
 
+// While it lives, memory for a call on a given stream comes from that stream's pool: the current stream may still have work before it that
+// uses what its own pool hands out, and the given stream waits for none of it.
+struct MemoryOf {
+    c10::cuda::OptionalCUDAStreamGuard on;
+    MemoryOf(PyObject *o, void *stream, c10::DeviceIndex device) {
+        if (given(o)) on.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, device));
+    }
+};
+
+// An output of such a call.
+at::Tensor new_output(PyObject *o, void *stream, at::IntArrayRef size, at::ScalarType dtype, const at::Tensor &like) {
+    const MemoryOf memory(o, stream, like.device().index());
+    return new_tensor(size, dtype, like);
+}
+
 // The scratch buffer of calls that bring none: one per device and purpose, as large as the largest call so far.  (Never
 // destroyed: the allocator may be gone when static objects are.)  Guarded by the GIL.
 std::map<std::pair<int, std::string>, at::Tensor> &workspaces() {
@@ -207,19 +222,19 @@ PyObject *mla_decode(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObje
     SPLASH_ASSERT(q->is_cuda() && q->scalar_type() == at::kBFloat16);
     int64_t first, last, flags;
     if (!integer(v[6], 0, first) || !integer(v[7], q->size(1), last) || !integer(v[14], 0, flags)) return nullptr;
+    void *stream;
+    if (!stream_of(v[13], stream)) return nullptr;
     at::Tensor out, lse;
     const int64_t B = q->size(0), H = q->size(1);
     if (given(v[10])) { const at::Tensor *t = tensor(v[10], "out"); if (!t) return nullptr; out = *t; }
-    else if (q->dim() == 4) out = new_tensor({B, H, q->size(2), kDV}, at::kFloat, *q);
-    else out = new_tensor({B, H, kDV}, at::kFloat, *q);
+    else if (q->dim() == 4) out = new_output(v[13], stream, {B, H, q->size(2), kDV}, at::kFloat, *q);
+    else out = new_output(v[13], stream, {B, H, kDV}, at::kFloat, *q);
     if (given(v[11])) { const at::Tensor *t = tensor(v[11], "lse"); if (!t) return nullptr; lse = *t; }
-    else if (q->dim() == 4) lse = new_tensor({B, H, q->size(2)}, at::kFloat, *q);
-    else lse = new_tensor({B, H}, at::kFloat, *q);
+    else if (q->dim() == 4) lse = new_output(v[13], stream, {B, H, q->size(2)}, at::kFloat, *q);
+    else lse = new_output(v[13], stream, {B, H}, at::kFloat, *q);
     SPLASH_ASSERT(table->scalar_type() == at::kInt && lens->scalar_type() == at::kInt);
     splash_mla_shape shape;
     if (!fill_shape(shape, *q, *kv, *table, out, lse, scale, flags)) return nullptr;
-    void *stream;
-    if (!stream_of(v[13], stream)) return nullptr;
     if (!ws) ws = &cached_workspace(*q, splash_mla_decode_workspace_bytes(&shape, (int32_t)first, (int32_t)last), "decode");
     const at::Tensor keep = *ws;                    // another thread may replace the cached one while the GIL is released
     const size_t ws_bytes = (size_t)keep.numel() * keep.element_size();
@@ -271,15 +286,15 @@ PyObject *mla_decode_sparse(PyObject *, PyObject *const *args, Py_ssize_t nargs,
     SPLASH_ASSERT(table->scalar_type() == at::kInt && lens->scalar_type() == at::kInt);
     int64_t most, first, last, flags;
     if (!integer(v[7], sel->size(1), most) || !integer(v[8], 0, first) || !integer(v[9], q->size(1), last) || !integer(v[14], 0, flags)) return nullptr;
-    at::Tensor out, lse;
-    if (given(v[10])) { const at::Tensor *t = tensor(v[10], "out"); if (!t) return nullptr; out = *t; }
-    else out = new_tensor({q->size(0), q->size(1), kDV}, at::kFloat, *q);
-    if (given(v[11])) { const at::Tensor *t = tensor(v[11], "lse"); if (!t) return nullptr; lse = *t; }
-    else lse = new_tensor({q->size(0), q->size(1)}, at::kFloat, *q);
-    splash_mla_shape shape;
-    if (!fill_shape(shape, *q, *kv, *table, out, lse, scale, flags)) return nullptr;
     void *stream;
     if (!stream_of(v[13], stream)) return nullptr;
+    at::Tensor out, lse;
+    if (given(v[10])) { const at::Tensor *t = tensor(v[10], "out"); if (!t) return nullptr; out = *t; }
+    else out = new_output(v[13], stream, {q->size(0), q->size(1), kDV}, at::kFloat, *q);
+    if (given(v[11])) { const at::Tensor *t = tensor(v[11], "lse"); if (!t) return nullptr; lse = *t; }
+    else lse = new_output(v[13], stream, {q->size(0), q->size(1)}, at::kFloat, *q);
+    splash_mla_shape shape;
+    if (!fill_shape(shape, *q, *kv, *table, out, lse, scale, flags)) return nullptr;
     if (!ws) {
         const size_t need = splash_mla_decode_sparse_workspace_bytes(&shape, (int32_t)most, (int32_t)first, (int32_t)last);
         if (need == 0) return raise_status(SPLASH_INVALID_ARG);
@@ -313,13 +328,13 @@ PyObject *lse_merge(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObjec
     SPLASH_ASSERT(po->is_contiguous() && pl->is_contiguous());
     if (po->dim() != 3) { PyErr_SetString(PyExc_ValueError, "part_out must be [parts][rows][d_v]"); return nullptr; }
     const int64_t parts = po->size(0), rows = po->size(1), dv = po->size(2);
-    at::Tensor out, lse;
-    if (given(v[2])) { const at::Tensor *t = tensor(v[2], "out"); if (!t) return nullptr; out = *t; }
-    else out = new_tensor({rows, dv}, at::kFloat, *po);
-    if (given(v[3])) { const at::Tensor *t = tensor(v[3], "lse"); if (!t) return nullptr; lse = *t; }
-    else lse = new_tensor({rows}, at::kFloat, *po);
     void *stream;
     if (!stream_of(v[4], stream)) return nullptr;
+    at::Tensor out, lse;
+    if (given(v[2])) { const at::Tensor *t = tensor(v[2], "out"); if (!t) return nullptr; out = *t; }
+    else out = new_output(v[4], stream, {rows, dv}, at::kFloat, *po);
+    if (given(v[3])) { const at::Tensor *t = tensor(v[3], "lse"); if (!t) return nullptr; lse = *t; }
+    else lse = new_output(v[4], stream, {rows}, at::kFloat, *po);
     const void *po_at = po->data_ptr(), *pl_at = pl->data_ptr();
     void *out_at = out.data_ptr(), *lse_at = lse.data_ptr();
     const int rc = without_gil([&] {
@@ -406,12 +421,12 @@ PyObject *dop_pack_rows(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyO
         SPLASH_ASSERT(b->size(0) == a->size(0) && b->size(1) == a->size(1));
         db = b->size(2);
     }
-    at::Tensor out;
-    if (given(v[3])) { const at::Tensor *t = tensor(v[3], "out"); if (!t) return nullptr; out = *t; }
-    else out = new_tensor({n, h, da + db}, a->scalar_type(), *a);
-    SPLASH_ASSERT(out.is_contiguous() && out.sizes() == at::IntArrayRef({n, h, da + db}));
     void *stream;
     if (!stream_of(v[4], stream)) return nullptr;
+    at::Tensor out;
+    if (given(v[3])) { const at::Tensor *t = tensor(v[3], "out"); if (!t) return nullptr; out = *t; }
+    else out = new_output(v[4], stream, {n, h, da + db}, a->scalar_type(), *a);
+    SPLASH_ASSERT(out.is_contiguous() && out.sizes() == at::IntArrayRef({n, h, da + db}));
     const void *a_at = a->data_ptr(), *b_at = ptr(b), *row_at = row->data_ptr();
     void *out_at = out.data_ptr();
     const int64_t a_row = a->stride(0) * es, a_head = a->stride(1) * es, b_row = b ? b->stride(0) * es : 0, b_head = b ? b->stride(1) * es : 0;
@@ -435,6 +450,8 @@ PyObject *dop_swap_outer(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
     SPLASH_ASSERT(x->is_contiguous() && x->dim() >= 2);
     int64_t inner = x->element_size();
     for (int64_t k = 2; k < x->dim(); ++k) inner *= x->size(k);
+    void *stream;
+    if (!stream_of(v[2], stream)) return nullptr;
     at::Tensor out;
     if (given(v[1])) {
         const at::Tensor *t = tensor(v[1], "out");
@@ -443,11 +460,9 @@ PyObject *dop_swap_outer(PyObject *, PyObject *const *args, Py_ssize_t nargs, Py
     } else {
         at::DimVector size(x->sizes().begin(), x->sizes().end());
         std::swap(size[0], size[1]);
-        out = new_tensor(size, x->scalar_type(), *x);
+        out = new_output(v[2], stream, size, x->scalar_type(), *x);
     }
     SPLASH_ASSERT(out.is_contiguous());
-    void *stream;
-    if (!stream_of(v[2], stream)) return nullptr;
     const void *x_at = x->data_ptr();
     void *out_at = out.data_ptr();
     const int64_t A = x->size(0), Bn = x->size(1);
@@ -512,15 +527,6 @@ bool stream_on(PyObject *o, c10::DeviceIndex device, void *&stream) {
     if (!given(o)) { stream = c10::cuda::getCurrentCUDAStream(device).stream(); return true; }
     return stream_of(o, stream);
 }
-
-// While it lives, memory for a call on a given stream comes from that stream's pool: the current stream may still have work before it that
-// uses what its own pool hands out, and the given stream waits for none of it.
-struct MemoryOf {
-    c10::cuda::OptionalCUDAStreamGuard on;
-    MemoryOf(PyObject *o, void *stream, c10::DeviceIndex device) {
-        if (given(o)) on.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)stream, device));
-    }
-};
 
 // A 1-D tensor over a part of another one's memory.
 at::Tensor part_of(const at::Tensor &all, int64_t byte, int64_t n, at::ScalarType dtype) {
