@@ -774,7 +774,9 @@ __device__ __forceinline__ void soften(const Block &b, int r /* row of the tile 
             ok = warp_wait(b.ctx, b.bar(kBarScale + (page & 3)), (page >> 2) & 1, kBarScale);
             if (!ok) break;
             float a = back * scales[2 * (page & 3)];
-            const float vs = scales[2 * (page & 3) + 1];
+            const int tb = start + u * kPage;
+            // (a row that sees no token of the page keeps its unit: the page's scale, which may be anything to it, does not move its O)
+            const float vs = tb < lim ? scales[2 * (page & 3) + 1] : 0.f;
             ok = warp_wait(b.ctx, b.bar(kBarS + buffer), (page >> 1) & 1, kBarS);
             if (!ok) break;
             tcgen05_fence_after();
@@ -784,12 +786,12 @@ __device__ __forceinline__ void soften(const Block &b, int r /* row of the tile 
                 tcgen05_fence_after();
                 rescale<D>(col_o, factor);
             };
-            if (fabsf(vs) > unit) {
-                if (u > 0) shrink(__fdividef(unit, fabsf(vs)));
-                unit = fabsf(vs);
+            const bool larger = fabsf(vs) > unit;
+            if (__any_sync(0xffffffffu, larger)) {
+                if (u > 0) shrink(larger ? __fdividef(unit, fabsf(vs)) : 1.f);
+                if (larger) unit = fabsf(vs);
             }
             const float f = vs == unit ? 1.f : __fdividef(vs, unit);
-            const int tb = start + u * kPage;
             if (tb < lo || tb + kPage > lim_min) a = hide(col, lo - tb, lim - tb, a);
             // y = x - ref, p = 2^y.  Whether a logit exceeds the reference by too much shows while the weights are computed; then they
             // are computed again (the weights' place is that of the sums: they are written when all of them are known to be right).
