@@ -8,7 +8,7 @@
 //   - 1 warp issues tcgen05.mma: S = Q K^T from shared memory into one of two buffers in tensor memory; O += P V with P read from tensor memory, where the
 //     softmax leaves it over S.  While the softmax has page u, S of page u + 1 is there and O of page u - 1 under way;
 //   - 4 softmax warps, a thread per row: p = 2^(x - m + 7) with a reference m that moves only when a logit exceeds it by 8 (then O and the sum are
-//     rescaled), p rounded to fp16, value scales folded into p as v_scale / U with U the largest so far;
+//     rescaled), p rounded to fp16, value scales folded into p as v_scale / U with U the largest so far of pages that the row sees;
 //   - 1 scheduler warp walks the worker's share of the cost line and publishes segments (an item's range of pages) and their pages ahead of the others.
 // Shared memory bounds it: a page costs 32 KB of stores, 16 KB for K and for V and 32 KB for Q, 768 cycles at 128 bytes, against 640 of MMAs and 512 of
 // exponentials (two chunks of 2,048 rows behind 8,192 tokens, 32 heads on 8 of 128: 517 us in a loop, 930 TFLOP/s, some 2,400 cycles a page

@@ -4,7 +4,7 @@
 // 16 (heads of 64: 32).  An item of work is (request, key head, tile); its pages are streamed once:
 //     x = q . K * softmax_scale * log2 e * k_scale,  p = 2^(x - m + 7),  l += p,  O += p * v_scale / U * V
 // with a reference m per row that moves only when a logit exceeds it by 8 (then O and l are rescaled) and U the largest
-// value scale so far.  p <= 2^15 is rounded to fp16 for the product with V: 11 bits, for weights down to 2^-21 of the largest.  Queries are scaled to
+// value scale so far, of the pages that the row sees.  p <= 2^15 is rounded to fp16 for the product with V: 11 bits, for weights down to 2^-21 of the largest.  Queries are scaled to
 // fp16's range by a power of two per row, so that bf16 ones lose nothing.
 //
 // The cache's bytes bound it, 16 KB a page and head of 128: one context of 262,144 tokens on eight key heads takes 92 us, 5.8 TB/s of the 6.5 that a copy
@@ -64,8 +64,9 @@ struct Layout {
     static constexpr int kMerge = kStages * 2 * kHalf;                     // [4][8][D + 4] fp32
     static constexpr int kQuery = kMerge + kConsumers * 8 * kPad * 4;      // [NT][D / 16][32] uint2
     static constexpr int kInfo = kQuery + (kQueryShared ? NT * (D / 16) * 256 : 0);
-    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // references, sums: [4][rows] each, two sets
-    static constexpr int kBars = kStats + 2 * 2 * kConsumers * kRows * 4;
+    static constexpr int kSet = (2 * kConsumers + 1) * kRows;              // references, sums: [4][rows] each; units: [rows]
+    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // two of these sets
+    static constexpr int kBars = kStats + 2 * kSet * 4;
     static constexpr int kBytes = kBars + (2 * kStages + 1) * 8 + 1024;    // (the start is aligned to 1,024)
 };
 
@@ -312,7 +313,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
     const PageInfo *const infos = reinterpret_cast<const PageInfo *>(smem + L::kInfo);
     float *const merge = reinterpret_cast<float *>(smem + L::kMerge);
     uint2 *const query = reinterpret_cast<uint2 *>(smem + L::kQuery);
-    // references and sums of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
+    // references, sums and units of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
     float *stat_m = reinterpret_cast<float *>(smem + L::kStats);
     const int n = lane >> 2, c = lane & 3;
     const int perm = D == 128 ? (n >> 1) | (n & 1) << 2 : n;
@@ -375,6 +376,10 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                     for (int x = 0; x < 4; ++x) o[nt][j][x] = 0.f;
             }
             unit = per_unit = 0.f;
+            if (warp == 0) {
+                if (lane < L::kRows) stat_m[2 * kConsumers * L::kRows + lane] = -1.f;
+                __syncwarp();
+            }
             if (kQueryShared && !meet(ctx, group_bar, group_phase, lane)) break;
         }
         if (!(flags & kEmpty)) {
@@ -425,13 +430,20 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
             if (fabsf(vs) > unit) {
                 per_unit = __fdividef(1.f, fabsf(vs));
                 const float a = unit * per_unit;
-                unit = fabsf(vs);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int j = 0; j < kM; ++j)
+                    for (int e = 0; e < 2; ++e) {
+                        // A row that sees no token of the page, nor of a later one: the page's scale may be anything to it.  Its O stays as it
+                        // is, and the unit that it has is noted (-1: the last one).
+                        const bool done = (flags & kCausal) && lim[nt][e] <= page.w;
+                        float *const own = stat_m + 2 * kConsumers * L::kRows + nt * 8 + 2 * c + e;
+                        if (done && warp == 0 && n == 0 && *own < 0.f) *own = unit;
+                        const float b = done ? 1.f : a;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) o[nt][j][x] *= a;
+                        for (int j = 0; j < kM; ++j) { o[nt][j][e] *= b; o[nt][j][2 + e] *= b; }
+                    }
+                unit = fabsf(vs);
             }
             const float f = vs == unit ? 1.f : vs * per_unit;
             uint32_t hidden = 0;                     // logits of tokens that the row does not see, a bit each
@@ -566,7 +578,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
         if (flags & (kLast | kEmpty)) {
             // ---- the four warps' parts of the item
             const int m0 = info.m0, pairs = info.pairs, row0 = info.row0, head = info.head, slot = info.slot;
-            float *const stat_l = stat_m + kConsumers * L::kRows;
+            float *const stat_l = stat_m + kConsumers * L::kRows, *const units = stat_l + kConsumers * L::kRows;
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);
 #pragma unroll
@@ -606,7 +618,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                     for (int w = 0; w < kConsumers; ++w) top = fmaxf(top, stat_m[w * L::kRows + r]);
 #pragma unroll
                     for (int w = 0; w < kConsumers; ++w) sum += stat_l[w * L::kRows + r] * fast_exp2(stat_m[w * L::kRows + r] - top);
-                    const float scale = sum == 0.f ? 0.f : unit / sum;
+                    const float scale = sum == 0.f ? 0.f : (units[r] < 0.f ? unit : units[r]) / sum;
                     const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
                     const int row = mm / p.group, g = head * p.group + mm - row * p.group;
 #pragma unroll
@@ -630,7 +642,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                 if (nt + 1 < NT && m0 + nt * 8 + 8 < pairs && !(ok = meet(ctx, group_bar, group_phase, lane))) break;
             }
             if (!ok) break;
-            stat_m = reinterpret_cast<float *>(smem + L::kStats) + (stat_m == reinterpret_cast<float *>(smem + L::kStats) ? 2 * kConsumers * L::kRows : 0);
+            stat_m = reinterpret_cast<float *>(smem + L::kStats) + (stat_m == reinterpret_cast<float *>(smem + L::kStats) ? L::kSet : 0);
         } else {
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);

@@ -19,9 +19,11 @@ def attend(cache, q, rows):
     return [t.double().cpu().numpy() for t in got], q_start
 
 
-# rows of one request each, and its context: the last page (or two) is hidden from the first rows.  Whole contexts and such as are cut and joined, one
-# tile of rows and several
+# rows of one request each, and its context: the last page (or two) is hidden from the first rows.  Few rows and many, whole contexts and such as are
+# cut and joined, one tile of rows and several
 CHUNKS = [([150], [200], 4), ([300, 70], [300, 75], 1), ([90], [9000], 2)]
+
+FEW = [([4], [66], 4), ([8, 3, 5], [70, 129, 5001], 2), ([8], [68], 3), ([5], [29955], 1), ([4, 4], [65, 130], 8), ([2, 2, 2], [65, 641, 1], 8)]
 
 
 def last_page_scaled(rows, lens, group, D, scale):
@@ -54,3 +56,30 @@ def test_rows_that_see_the_page_have_its_scale(rows, lens, group, D):
     # 2^100: what the other pages add to such a row is below its rounding
     cache, q, q_start, got = last_page_scaled(rows, lens, group, D, 2.0 ** 100)
     _kv8.check(got, _kv8.attention(cache, q.double().numpy(), q_start, 1 / math.sqrt(D), out_eps=2.0 ** -24))
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 60, 2.0 ** 115, -1e38, 3e38, np.inf, np.nan, 0.0, 1e-40])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows,lens,group", FEW)
+def test_few_rows(rows, lens, group, D, scale):
+    last_page_scaled(rows, lens, group, D, scale)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows,lens,group", FEW)
+def test_few_rows_that_see_the_page_have_its_scale(rows, lens, group, D):
+    cache, q, q_start, got = last_page_scaled(rows, lens, group, D, 2.0 ** 100)
+    _kv8.check(got, _kv8.attention(cache, q.double().numpy(), q_start, 1 / math.sqrt(D), out_eps=2.0 ** -24))
+
+
+@pytest.mark.parametrize("most", [40, 90])
+def test_several_pages_behind_a_row(most):
+    # of 150 announced rows at the positions from 150 on the first `most` are computed: the last pages, from 192 and 256 on, are hidden from all or some of them
+    cache = _kv8.Cache(42, [300], 1, 64)
+    q = torch.from_numpy(np.random.default_rng(42).normal(size=(150, 1, 64))).to(torch.bfloat16)
+    ref = [a.copy() for a in _kv8.attention(cache, q.double().numpy(), [0, 150], 0.125, out_eps=2.0 ** -24)]
+    cache.scales[1][cache.table[0, 3]], cache.scales[1][cache.table[0, 4]] = 1e38, 3e38
+    out, lse = torch.empty((150, 1, 64), device="cuda"), torch.empty((150, 1), device="cuda")
+    B.splash_kv8_attention(q.cuda(), *cache.cuda(), softmax_scale=0.125, q_start=torch.tensor([0, 150], dtype=torch.int32, device="cuda"), max_q_rows=most, out=out, lse=lse)
+    blind = slice(0, 192 - 150 if most > 42 else most)
+    _kv8.check((out[blind].double().cpu().numpy(), lse[blind].cpu().numpy()), [a[blind] for a in ref])
