@@ -502,7 +502,7 @@ typedef struct splash_kv8_query {
  * or num_rows alike.
  *
  * Only tokens in R enter a row's result: codes of the cache's other places, and scales of pages without a token of R, may be
- * anything, NaN included; NaN in a token's data stays NaN in the rows that attend it.  A page id outside the
+ * anything, NaN included; NaN in a token's data stays NaN in the rows that attend it (a scale that is infinite counts as NaN).  A page id outside the
  * cache is never dereferenced, the page reads as zeros.  Products are exact (8-bit codes times q, which is scaled to fp16's range by a power of two per
  * row) and summed in fp32; softmax weights are rounded to fp16 relative to the row's running maximum, maxima and sums are
  * fp32.  Value scales that differ by up to 2^20 between the pages of a request keep that precision.  Results are bit-reproducible for a fixed call.

@@ -503,8 +503,8 @@ __device__ __forceinline__ void convert_keys(const Block &b, int tid, int lane) 
         if (!warp_wait(b.ctx, b.bar(kBarKEmpty + stage), ((page >> 1) & 1) ^ 1, kBarKEmpty)) return;
         codes.store(b.smem + L::kK + stage * L::kTile, tid);
         if (tid == 0) {
-            const float vs = now->v_scale;
-            scales[2 * turn] = now->k_scale;
+            const float ks = now->k_scale, vs = now->v_scale;
+            scales[2 * turn] = isfinite(ks) ? ks : NAN;      // (keys that are infinite, with either sign: their logit is no number)
             scales[2 * turn + 1] = isfinite(vs) ? vs : now->flags & kPageEdge ? 0.f : NAN;
             mbar_arrive(b.bar(kBarScale + turn));
         }

@@ -304,6 +304,8 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     return r;
 }
 
+__device__ __forceinline__ float number(float x) { return fabsf(x) == INFINITY ? NAN : x; }
+
 template <int D, int NT>
 __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint32_t bars, const Ctx &ctx, int warp, int lane) {
     using L = Layout<D, NT>;
@@ -426,7 +428,8 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                 }
             }
             // ---- weights, in base 2 relative to the row's reference, and relative to the largest value scale so far
-            const float ks = __int_as_float(page.y), scale = __int_as_float(page.z), vs = fabsf(scale) == INFINITY ? NAN : scale;
+            // (an infinite scale counts as NaN: keys that are infinite, with either sign, have a logit that is no number)
+            const float ks = number(__int_as_float(page.y)), vs = number(__int_as_float(page.z));
             if (fabsf(vs) > unit) {
                 per_unit = __fdividef(1.f, fabsf(vs));
                 const float a = unit * per_unit;
