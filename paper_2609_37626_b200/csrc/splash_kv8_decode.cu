@@ -64,9 +64,8 @@ struct Layout {
     static constexpr int kMerge = kStages * 2 * kHalf;                     // [4][8][D + 4] fp32
     static constexpr int kQuery = kMerge + kConsumers * 8 * kPad * 4;      // [NT][D / 16][32] uint2
     static constexpr int kInfo = kQuery + (kQueryShared ? NT * (D / 16) * 256 : 0);
-    static constexpr int kSet = (2 * kConsumers + 1) * kRows;              // references, sums: [4][rows] each; units: [rows]
-    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // two of these sets
-    static constexpr int kBars = kStats + 2 * kSet * 4;
+    static constexpr int kStats = kInfo + kStages * (int)sizeof(PageInfo); // references, sums: [4][rows] each, two sets
+    static constexpr int kBars = kStats + 2 * 2 * kConsumers * kRows * 4;
     static constexpr int kBytes = kBars + (2 * kStages + 1) * 8 + 1024;    // (the start is aligned to 1,024)
 };
 
@@ -306,6 +305,20 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 
 __device__ __forceinline__ float number(float x) { return fabsf(x) == INFINITY ? NAN : x; }
 
+// What a row that is done is multiplied with where the unit grows from `from` to `to`: its result O * unit / l stays, and so does its sum, with l times
+// 2^shift and the reference less by that.  Three eighths of the growth go to l and the rest to O, however many steps it takes, so that neither leaves
+// fp32's range (l is below 2^45, O in the order of 2^7; from 2^-7 to 2^127 l grows by 2^50 and O falls by 2^84).
+struct Done { float o, l, shift; };
+__device__ __forceinline__ Done done_row(float from, float to) {
+    const int a = __float_as_int(from), b = __float_as_int(to), grown = (b >> 23) - (a >> 23), shift = (3 * (b >> 23) >> 3) - (3 * (a >> 23) >> 3);
+    const float mantissas = __fdividef(__int_as_float((a & 0x7fffff) | 0x3f800000), __int_as_float((b & 0x7fffff) | 0x3f800000));
+    Done d;
+    d.o = from == 0.f ? 0.f : mantissas * __int_as_float(max(127 - (grown - shift), 0) << 23);
+    d.l = __int_as_float((127 + shift) << 23);
+    d.shift = (float)shift;
+    return d;
+}
+
 template <int D, int NT>
 __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint32_t bars, const Ctx &ctx, int warp, int lane) {
     using L = Layout<D, NT>;
@@ -315,7 +328,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
     const PageInfo *const infos = reinterpret_cast<const PageInfo *>(smem + L::kInfo);
     float *const merge = reinterpret_cast<float *>(smem + L::kMerge);
     uint2 *const query = reinterpret_cast<uint2 *>(smem + L::kQuery);
-    // references, sums and units of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
+    // references and sums of the warps' rows, in two sets by turns: a warp may be at the end of the next item while another still reads these
     float *stat_m = reinterpret_cast<float *>(smem + L::kStats);
     const int n = lane >> 2, c = lane & 3;
     const int perm = D == 128 ? (n >> 1) | (n & 1) << 2 : n;
@@ -378,10 +391,6 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                     for (int x = 0; x < 4; ++x) o[nt][j][x] = 0.f;
             }
             unit = per_unit = 0.f;
-            if (warp == 0) {
-                if (lane < L::kRows) stat_m[2 * kConsumers * L::kRows + lane] = -1.f;
-                __syncwarp();
-            }
             if (kQueryShared && !meet(ctx, group_bar, group_phase, lane)) break;
         }
         if (!(flags & kEmpty)) {
@@ -433,19 +442,26 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
             if (fabsf(vs) > unit) {
                 per_unit = __fdividef(1.f, fabsf(vs));
                 const float a = unit * per_unit;
+                if (!(flags & kCausal)) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        // A row that sees no token of the page, nor of a later one: the page's scale may be anything to it.  Its O stays as it
-                        // is, and the unit that it has is noted (-1: the last one).
-                        const bool done = (flags & kCausal) && lim[nt][e] <= page.w;
-                        float *const own = stat_m + 2 * kConsumers * L::kRows + nt * 8 + 2 * c + e;
-                        if (done && warp == 0 && n == 0 && *own < 0.f) *own = unit;
-                        const float b = done ? 1.f : a;
+                        for (int j = 0; j < kM; ++j)
 #pragma unroll
-                        for (int j = 0; j < kM; ++j) { o[nt][j][e] *= b; o[nt][j][2 + e] *= b; }
-                    }
+                            for (int x = 0; x < 4; ++x) o[nt][j][x] *= a;
+                } else {
+                    // (a row that sees no token of the page, nor of a later one, is done: the page's scale may be anything to it)
+                    const Done done = done_row(unit, fabsf(vs));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float b = a;
+                            if (lim[nt][e] <= page.w) { b = done.o; l[nt][e] *= done.l; ref[nt][e] -= done.shift; }
+#pragma unroll
+                            for (int j = 0; j < kM; ++j) { o[nt][j][e] *= b; o[nt][j][2 + e] *= b; }
+                        }
+                }
                 unit = fabsf(vs);
             }
             const float f = vs == unit ? 1.f : vs * per_unit;
@@ -581,7 +597,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
         if (flags & (kLast | kEmpty)) {
             // ---- the four warps' parts of the item
             const int m0 = info.m0, pairs = info.pairs, row0 = info.row0, head = info.head, slot = info.slot;
-            float *const stat_l = stat_m + kConsumers * L::kRows, *const units = stat_l + kConsumers * L::kRows;
+            float *const stat_l = stat_m + kConsumers * L::kRows;
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);
 #pragma unroll
@@ -621,8 +637,11 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                     for (int w = 0; w < kConsumers; ++w) top = fmaxf(top, stat_m[w * L::kRows + r]);
 #pragma unroll
                     for (int w = 0; w < kConsumers; ++w) sum += stat_l[w * L::kRows + r] * fast_exp2(stat_m[w * L::kRows + r] - top);
-                    const float scale = sum == 0.f ? 0.f : (units[r] < 0.f ? unit : units[r]) / sum;
-                    const float lse2 = sum == 0.f ? -INFINITY : top + __log2f(sum);
+                    const float scale = sum == 0.f ? 0.f : unit / sum;
+                    // (the sum's exponent goes to the reference, exactly: of its logarithm a mantissa's is left)
+                    const int sum_bits = __float_as_int(sum);
+                    const float mantissa = __int_as_float((sum_bits & 0x7fffff) | 0x3f800000);
+                    const float lse2 = sum == 0.f ? -INFINITY : sum < INFINITY ? top + (float)((sum_bits >> 23) - 127) + __log2f(mantissa) : sum;
                     const int row = mm / p.group, g = head * p.group + mm - row * p.group;
 #pragma unroll
                     for (int q = 0; q < D / 64; ++q) {
@@ -645,7 +664,7 @@ __device__ __forceinline__ void consume(const AttnParams &p, uint8_t *smem, uint
                 if (nt + 1 < NT && m0 + nt * 8 + 8 < pairs && !(ok = meet(ctx, group_bar, group_phase, lane))) break;
             }
             if (!ok) break;
-            stat_m = reinterpret_cast<float *>(smem + L::kStats) + (stat_m == reinterpret_cast<float *>(smem + L::kStats) ? L::kSet : 0);
+            stat_m = reinterpret_cast<float *>(smem + L::kStats) + (stat_m == reinterpret_cast<float *>(smem + L::kStats) ? 2 * kConsumers * L::kRows : 0);
         } else {
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * stage);

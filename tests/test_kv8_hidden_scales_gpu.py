@@ -72,13 +72,14 @@ def test_few_rows_that_see_the_page_have_its_scale(rows, lens, group, D):
     _kv8.check(got, _kv8.attention(cache, q.double().numpy(), q_start, 1 / math.sqrt(D), out_eps=2.0 ** -24))
 
 
+@pytest.mark.parametrize("scales", [(1e38, 3e38), (2.0 ** 53, 2.0 ** 113), (3e38, 1.0), (2.0 ** -3, 2.0 ** 126)])
 @pytest.mark.parametrize("most", [40, 90])
-def test_several_pages_behind_a_row(most):
+def test_several_pages_behind_a_row(most, scales):
     # of 150 announced rows at the positions from 150 on the first `most` are computed: the last pages, from 192 and 256 on, are hidden from all or some of them
     cache = _kv8.Cache(42, [300], 1, 64)
     q = torch.from_numpy(np.random.default_rng(42).normal(size=(150, 1, 64))).to(torch.bfloat16)
     ref = [a.copy() for a in _kv8.attention(cache, q.double().numpy(), [0, 150], 0.125, out_eps=2.0 ** -24)]
-    cache.scales[1][cache.table[0, 3]], cache.scales[1][cache.table[0, 4]] = 1e38, 3e38
+    cache.scales[1][cache.table[0, 3]], cache.scales[1][cache.table[0, 4]] = scales
     out, lse = torch.empty((150, 1, 64), device="cuda"), torch.empty((150, 1), device="cuda")
     B.splash_kv8_attention(q.cuda(), *cache.cuda(), softmax_scale=0.125, q_start=torch.tensor([0, 150], dtype=torch.int32, device="cuda"), max_q_rows=most, out=out, lse=lse)
     blind = slice(0, 192 - 150 if most > 42 else most)
