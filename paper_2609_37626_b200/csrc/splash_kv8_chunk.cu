@@ -924,14 +924,14 @@ cudaError_t launch_chunk(const AttnParams &p, const splash_kv8_cache &cache, cud
 
 }  // namespace
 
-cudaError_t launch_kv8_combine(const AttnParams &p, int D, int rows, int items, cudaStream_t stream);     // (of the decode path)
+cudaError_t launch_kv8_chunk_combine(const AttnParams &p, int D, cudaStream_t stream);     // (with the combine kernel of the decode path)
 
 int kv8_chunk_rows() { return kTileRows; }
 int kv8_chunk_workers(int sm_count) { return 2 * sm_count; }
 
 cudaError_t launch_kv8_chunk(const AttnParams &p, const splash_kv8_cache &cache, cudaStream_t stream) {
     cudaError_t e = cache.head_dim == 128 ? launch_chunk<128>(p, cache, stream) : launch_chunk<64>(p, cache, stream);
-    if (e == cudaSuccess && !p.whole) e = launch_kv8_combine(p, cache.head_dim, kTileRows, p.workers, stream);
+    if (e == cudaSuccess && !p.whole) e = launch_kv8_chunk_combine(p, cache.head_dim, stream);
     return e;
 }
 

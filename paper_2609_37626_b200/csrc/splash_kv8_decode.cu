@@ -808,23 +808,23 @@ bool make_pool_map(CUtensorMap *map, const splash_kv8_cache &c, const void *pool
     return r == CUDA_SUCCESS;
 }
 
-// `items`: no more of them are cut
-template <int D, int kRows>
-cudaError_t launch_combine(const AttnParams &p, int items, cudaStream_t stream) {
+template <int D, int kRows, int kWarps>
+cudaError_t launch_combine_of(const AttnParams &p, cudaStream_t stream) {
     static DeviceOnce once;
     cudaError_t e = once.run([] {
         // (an SM that had to change its shared memory between the two kernels would have to run empty first)
-        for (const auto kernel : {kv8_combine_kernel<D, kRows, 1>, kv8_combine_kernel<D, kRows, 4>}) {
-            const cudaError_t c = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-            if (c != cudaSuccess) return c;
-        }
-        return cudaSuccess;
+        return cudaFuncSetAttribute(kv8_combine_kernel<D, kRows, kWarps>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     });
     if (e != cudaSuccess) return e;
-    e = p.workers / items >= 8 ? launch_dependent(kv8_combine_kernel<D, kRows, 4>, dim3(p.workers, kRows), dim3(128), 0, stream, p)
-                               : launch_dependent(kv8_combine_kernel<D, kRows, 1>, dim3(p.workers, kRows / 4), dim3(128), 0, stream, p);
+    e = launch_dependent(kv8_combine_kernel<D, kRows, kWarps>, dim3(p.workers, kRows * kWarps / 4), dim3(128), 0, stream, p);
     count_launch();
     return e;
+}
+
+// `items`: no more of them are cut
+template <int D, int kRows>
+cudaError_t launch_combine(const AttnParams &p, int items, cudaStream_t stream) {
+    return p.workers / items >= 8 ? launch_combine_of<D, kRows, 4>(p, stream) : launch_combine_of<D, kRows, 1>(p, stream);
 }
 
 template <int D, int NT>
@@ -856,10 +856,9 @@ bool kv8_pool_maps(const splash_kv8_cache &c, CUtensorMap *k_map, CUtensorMap *v
     return make_pool_map(k_map, c, c.k_pool, c.k_page_stride, c.k_head_stride) && make_pool_map(v_map, c, c.v_pool, c.v_page_stride, c.v_head_stride);
 }
 
-// of the kernel for many rows
-cudaError_t launch_kv8_combine(const AttnParams &p, int D, int rows, int items, cudaStream_t stream) {
-    if (rows != 128) return cudaErrorInvalidValue;
-    return D == 128 ? launch_combine<128, 128>(p, items, stream) : launch_combine<64, 128>(p, items, stream);
+// of the kernel for many rows: a warp to a row, whatever is cut
+cudaError_t launch_kv8_chunk_combine(const AttnParams &p, int D, cudaStream_t stream) {
+    return D == 128 ? launch_combine_of<128, 128, 1>(p, stream) : launch_combine_of<64, 128, 1>(p, stream);
 }
 
 cudaError_t launch_kv8_decode(const AttnParams &p, int D, int rows, const CUtensorMap &k_map, const CUtensorMap &v_map, cudaStream_t stream) {
