@@ -12,6 +12,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <map>
 #include <string>
 #include <utility>
@@ -560,6 +561,9 @@ PyObject *kv_slots(PyObject *, PyObject *const *args, Py_ssize_t nargs, PyObject
     const c10::cuda::CUDAGuard guard(table->device());
     void *stream;
     if (!stream_on(v[11], table->device().index(), stream)) return nullptr;
+    if (B > SPLASH_KV_SLOTS_MAX_REQUESTS || places > 0x7ffffffe)        // (refused, before memory for the outputs is asked for)
+        return raise_status(splash_kv_slots((int32_t)std::min<int64_t>(B, INT32_MAX), nullptr, nullptr, nullptr, 0, nullptr, nullptr, 0, 0, places, nullptr, nullptr,
+                                            nullptr, nullptr, nullptr, stream));
     const MemoryOf memory(v[11], stream, table->device().index());
     const int64_t sizes[5] = {places, places, B + 1, B, 4};
     at::Tensor out[5], all;
