@@ -478,7 +478,8 @@ SPLASH_API int splash_kv8_append(const splash_kv8_cache *cache, int32_t dtype, i
 typedef struct splash_kv8_query {
     uint32_t struct_size;        /* sizeof(splash_kv8_query) */
     int32_t num_requests;        /* B >= 0 */
-    int64_t num_rows;            /* T: rows of q, out and lse; below 2^31 */
+    int64_t num_rows;            /* T: rows of q, out and lse; below 2^31.  (Rows of no request are not computed; but from T near num_requests * max_q_rows
+                                    the call is laid out for requests of many rows each, and takes longer where most have few) */
     int32_t num_heads;           /* a multiple of the cache's num_kv_heads, at most 1,024 heads for each; head g reads key head g / (num_heads / num_kv_heads) */
     int32_t max_q_rows;          /* upper bound on the rows of a request, >= 1 */
     int32_t dtype;               /* of q: SPLASH_DTYPE_BF16 or SPLASH_DTYPE_FP16 */

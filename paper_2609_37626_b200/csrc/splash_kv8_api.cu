@@ -97,9 +97,12 @@ View carve(void *base, int workers, int rows, int D) {
     return v;
 }
 
-// How a call runs: requests of up to this many (row, head) pairs on the decode kernel, the others, if there may be any, on the kernel for chunks, which
-// takes 128 pairs for about what the former takes for two of its tiles (64 contexts of 4,096 tokens, eight key heads of 128: 32 pairs 218 and 188 us, but four of them 27 and 30, 64 pairs 411
-// and 191; of 64, whose tiles hold twice the pairs: 48 pairs 178 and 143, 32 pairs 134 and about as much).
+// How a call runs: requests of up to this many (row, head) pairs on the decode kernel, the others, if there may be any, on the kernel for chunks.  What the
+// two take, in us, for contexts of 4,096 tokens and eight key heads (decode / chunks):
+//     heads of 128   64 contexts: 16 pairs 119 / 175, 24 215 / 177, 32 223 / 178     16 contexts: 44 / 62, 64 / 62, 66 / 63     four: 22.5 / 27, 26 / 27.5, 26 / 27.5
+//     heads of 64    64 contexts: 24 pairs 101 / 133, 32 135 / 135, 40 179 / 136     16 contexts: 34 / 46, 46 / 46, 54 / 47     four: 23 / 24, 30 / 24, 24 / 24
+// 64 pairs of 128 are 411 / 185 with 64 contexts.  So the limits suit few contexts; of many, the chunk kernel has 17 to 32 pairs of 128 and 33 to 40 of 64 done
+// sooner.  Pairs alone do not tell the two apart: the work of a block would have to come into it.
 int decode_pairs(const splash_kv8_cache *c) { return c->head_dim == 64 ? 40 : 32; }
 
 constexpr int64_t kMaxTokens = 1LL << 30;      // of a context: positions and page ends stay in 32 bits
@@ -115,8 +118,10 @@ Plan plan_call(const splash_kv8_cache *c, const splash_kv8_query *s, int sms) {
     const int64_t cost = (pairs + p.rows - 1) / p.rows * c->num_kv_heads * s->num_requests * (s->table_width + 5LL);
     if (cost > 0 && cost < p.workers) p.workers = (int)cost;
     p.chunk_workers = p.pairs > decode_pairs(c) ? kv8_chunk_workers(sms) : 0;
-    // With T rows in all and at most R for a request, at most (B R - T) / (R - 1) requests have a single one.  Where that is a quarter of them or less (a step of
-    // a fixed number of rows, one prompt), the kernel for chunks takes them all: two launches less, 6 us of such a call.
+    // How many requests have few rows only the device knows.  If all of the T rows belong to requests, of at most R each, (B R - T) / (R - 1) of them at most have a
+    // single one.  Where that is a quarter of them or less (a step of a fixed number of rows, one prompt), the kernel for chunks takes them all: two launches less,
+    // 6 us of such a call.  It is a guess: with rows of nobody among the T (a batch padded to B R rows), or rows beyond R, there may be more, and they take the
+    // slower kernel, with the same results (64 contexts of 4,096 tokens, eight heads a key head, a row each: 172 us with T = B R = 512 where 125 with T = 64).
     p.decode = p.chunk_workers == 0 || (int64_t)s->num_requests * s->max_q_rows - s->num_rows > (s->max_q_rows - 1LL) * s->num_requests / 4;
     return p;
 }
