@@ -506,7 +506,7 @@ typedef struct splash_kv8_query {
  * anything, NaN included; NaN in a token's data stays NaN in the rows that attend it (a scale that is infinite counts as NaN).  A page id outside the
  * cache is never dereferenced, the page reads as zeros.  Products are exact (8-bit codes times q, which is scaled to fp16's range by a power of two per
  * row) and summed in fp32; softmax weights are rounded to fp16 relative to the row's running maximum, maxima and sums are
- * fp32.  Value scales that differ by up to 2^20 between the pages of a request keep that precision.  Results are bit-reproducible for a fixed call.
+ * fp32.  Value scales below 2^126 that differ by up to 2^20 between the pages that a row sees keep that precision.  Results are bit-reproducible for a fixed call.
  * out and lse must not overlap each other, q or the cache.
  *
  *   block_table  [num_requests][block_table_stride] int32;  seq_lens, kv_begin, kv_end [num_requests] int32 (the latter two

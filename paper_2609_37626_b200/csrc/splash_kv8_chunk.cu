@@ -11,8 +11,8 @@
 //     rescaled), p rounded to fp16, value scales folded into p as v_scale / U with U the largest so far of pages that the row sees;
 //   - 1 scheduler warp walks the worker's share of the cost line and publishes segments (an item's range of pages) and their pages ahead of the others.
 // Shared memory bounds it: a page costs 32 KB of stores, 16 KB for K and for V and 32 KB for Q, 768 cycles at 128 bytes, against 640 of MMAs and 512 of
-// exponentials (two chunks of 2,048 rows behind 8,192 tokens, 32 heads on 8 of 128: 517 us in a loop, 930 TFLOP/s, some 2,400 cycles a page
-// and block, of which two run).
+// exponentials (two chunks of 2,048 rows behind 8,192 tokens, 32 heads on 8 of 128: 521 us a call in a loop, 925 TFLOP/s, 16 of them the join; some 2,450 cycles a page and
+// block, of which two run.  The first call after a pause takes 585: the same cycles, but at 1.69 GHz; by the tenth 525).
 // The line counts pages up to the tile's last causal row, and kOverhead per item (queries, epilogue); items cut by a share's end are joined by the
 // combine kernel of the decode path.
 #include "splash_kv8.cuh"

@@ -9,7 +9,7 @@
 //
 // The cache's bytes bound it, 16 KB a page and head of 128: one context of 262,144 tokens on eight key heads takes 92 us, 5.8 TB/s of the 6.5 that a copy
 // has; 64 contexts of 1k to 8k tokens 103 us, 5.9 TB/s; from 24 pairs on the MMAs and conversions do (heads of 128, 64 contexts of 4,096 tokens: 8 pairs 92 us,
-// 16 pairs 118, 24 and 32 pairs 212).  What it takes to stay there:
+// 16 pairs 119, 24 pairs 215, 32 pairs 223).  What it takes to stay there:
 //   - items are cut where the cost line (pages, and kOverhead per item) of all requests passes a worker's share, so one long
 //     context and 512 short ones fill the SMs alike; cut items are joined by a combine kernel.  Three workers per SM;
 //   - a producer warp walks the line, 32 pages at once: a lane each finds its page, its scales and its flags; TMA brings
@@ -843,9 +843,10 @@ cudaError_t launch_decode(const AttnParams &p, int items, const CUtensorMap &k_m
 
 }  // namespace
 
-// Rows of a tile for requests of at most `pairs` (row, head) pairs, and the workers that the line is cut for (the blocks that the GPU holds).  More rows
-// than 16 of 128 dimensions do not fit the registers of three blocks an SM (32: 47 us where two tiles of 16 take 37); of 64 dimensions 24 rows as one tile
-// take 37 us, as two of 16 as much, 32 rows 132 as one tile and 146 as two.
+// Rows of a tile for requests of at most `pairs` (row, head) pairs, and the workers that the line is cut for (the blocks that the GPU holds).  Three
+// blocks an SM leave 128 registers, which only tiles of eight rows, and of 16 rows of 64 dimensions, keep to.  16 rows of 128 dimensions spill 116 bytes, 24 and 32 rows of 64
+// dimensions 76 and 348; more than 16 of 128 dimensions cost more than the second tile (32: 47 us where two of 16 take 37), 24 rows of 64 dimensions as one
+// tile as much as two of 16 (37 us), 32 rows 135 us as one tile and 146 as two.
 void kv8_decode_shape(int64_t pairs, int head_dim, int sm_count, int *rows, int *workers) {
     const int64_t most = head_dim == 64 ? 32 : 16, tiles = (pairs + most - 1) / most;
     *rows = (int)((pairs + tiles - 1) / tiles + 7) / 8 * 8;
